@@ -1,6 +1,6 @@
 /* pipad.h - C ABI of the frame-parallel GCN aggregation library for AMD MI355X (gfx950).
  *
- * The library implements one thing: neighbour aggregation of a GCN layer over a frame (sliding
+ * The library implements neighbour aggregation of a GCN layer over a frame (sliding
  * window) of k graph snapshots, the way PiPAD's "dimension-aware parallel GNN" organises it
  * (Section 4.2): the topology of the snapshot group is regrouped as ONE overlap part shared by all
  * k snapshots plus one exclusive part per snapshot (Section 4.1, "Overlap-aware data transfer");
@@ -12,6 +12,9 @@
  *
  * (Eq. 1 of Section 2.1 aggregates over N(v) united with {v}; the normalisation is the symmetric
  * GCN one).  A_t is a 0/1 pattern; self-loops are implicit and never stored.
+ * Around the aggregations of a deeper model stand the operators on node rows (further down): norms before
+ * and after a block with its gate and residual scale, and the gated feed-forward block, each with its
+ * gradients, for the matrices of all k snapshots at once.
  *
  * Conventions that hold for every call
  *  - All array arguments named "device" are pointers into GPU memory of the CURRENT HIP device;
@@ -42,7 +45,8 @@ typedef enum pipad_status {
   PIPAD_ERR_ALLOC = -3,       /* device allocation failed (callback returned NULL / hipMalloc)  */
   PIPAD_ERR_TOO_LARGE = -4,   /* a size does not fit the int32 index space                      */
   PIPAD_ERR_HIP = -5,         /* a HIP runtime call failed; see pipad_last_hip_error()          */
-  PIPAD_ERR_SCRATCH = -6      /* the partial sums of this frame and F do not fit the scratch     *
+  PIPAD_ERR_SCRATCH = -6      /* the workspace given is too small; or                            *
+                               * the partial sums of this frame and F do not fit the scratch     *
                                * buffer and it cannot grow now (pipad_frame_aggregate_static; any *
                                * aggregation under stream capture); nothing was enqueued         */
 } pipad_status;
@@ -265,6 +269,108 @@ int pipad_frame_transpose(const pipad_frame_t *frame, pipad_alloc_fn alloc, void
 
 /* Releases the frame and every buffer the library allocated itself.  NULL is allowed. */
 void pipad_frame_destroy(pipad_frame_t *frame);
+
+/* ---- operators on node rows --------------------------------------------------------------------
+ * What a model does to the rows of the k feature matrices between two aggregations.  They need no frame: n rows in each
+ * of k matrices (1 <= k <= PIPAD_MAX_K, n >= 0; a single row is n = k = 1), given as host arrays of k device pointers with a
+ * row stride each, as for pipad_frame_aggregate (base + t*F with stride k*F is the concatenated operand).  The arrays and
+ * the structs only need to live for the duration of the call; vectors and weights are device memory, and so is `workspace`.
+ *  - The calls only enqueue kernels on `stream`: no allocation, no host synchronisation, so they can be recorded into a HIP
+ *    graph at any time.  `workspace` (16-byte aligned, at least as many bytes as the size query says for the same struct, n and
+ *    k; NULL where that is 0) holds nothing between calls and need not be cleared.  Calls that may run at the same time, replays of
+ *    recorded ones among them, need one each; too small a one is PIPAD_ERR_SCRATCH, with nothing enqueued.
+ *  - All pointers are of the current HIP device.  Matrices need no more than the alignment of a float, and no certain stride; rows
+ *    on 16-byte boundaries (base, and stride a multiple of 4) are read and written 16 bytes at a time where all of a call's are.
+ *  - Columns behind a row's last are neither read nor written; rows of results are written once; outputs must not overlap each
+ *    other or inputs, but where a comment says so.
+ *  - Results are deterministic: same inputs, strides and alignment, same bits.  Sums are 32-bit floats or more.
+ *  - PIPAD_ERR_TOO_LARGE: n times a stride of 2^40 or more, and the widths given below. */
+
+/* P = post(B),  R' = R + scale * sigmoid(gate) * P,  Z = pre(R')
+ * The norm after a block whose output is B, the block's gate and residual scale, and the norm before the next block, in one pass.
+ *   post, pre   PIPAD_NORM_NONE: left as it is (pre: no Z);  PIPAD_NORM_RMS: x / sqrt(mean(x^2) + eps);
+ *               PIPAD_NORM_LAYER: (x - mean(x)) / sqrt(var(x) + eps), the variance over F;  means are over a row's F columns,
+ *               eps >= 0 (a row of equal values under eps = 0 gives what 0 / 0 gives)
+ *   w_post, b_post, w_pre, b_pre   float [F], weight and bias behind each norm, NULL: 1 and 0; NULL where there is no norm
+ *   scale       float [F], the residual scale of each column, NULL: 1 */
+#define PIPAD_NORM_NONE 0
+#define PIPAD_NORM_RMS 1
+#define PIPAD_NORM_LAYER 2
+#define PIPAD_NORM_MAX_F 4096 /* longest row */
+typedef struct pipad_residual_norm_params {
+  int32_t F;
+  int32_t post, pre;
+  float eps;
+  const float *scale, *w_post, *b_post, *w_pre, *b_pre;
+} pipad_residual_norm_t;
+
+/*   R           the residual stream
+ *   B, gate     the block's output and its gate's input; gate NULL: no gate (a factor of 1); B NULL: no block, R' is R (then gate and
+ *               R_out are NULL, post PIPAD_NORM_NONE and scale NULL): the norm before a first block
+ *   R_out       receives R'; may be R itself (same pointers, same stride).  NULL: not wanted
+ *   Z           receives Z; NULL: not wanted (PIPAD_NORM_NONE: has to be NULL).  One of R_out and Z has to be there */
+int pipad_residual_norm(const pipad_residual_norm_t *norm, int32_t n, int32_t k, const float *const *R, int64_t ldr,
+                        const float *const *B, int64_t ldb, const float *const *gate, int64_t ldg, float *const *R_out,
+                        int64_t ldro, float *const *Z, int64_t ldz, void *stream);
+
+/* Gradients of the shared vectors, float [F] each, NULL: not wanted; written, not added to. */
+typedef struct pipad_residual_norm_grads {
+  float *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
+} pipad_residual_norm_grads_t;
+
+/* The gradients of pipad_residual_norm.
+ *   R           R' as the forward call gave it (B NULL: its R); with B and gate everything else is made again
+ *   dR_out, dZ  gradients of R' and Z; NULL: 0 (not both).  pre = PIPAD_NORM_NONE: dZ has to be NULL
+ *   dR          receives the gradient of R; may be dR_out itself (same pointers, same stride)
+ *   dB, dgate   receive those of B and gate.  All three may be NULL: not wanted
+ *   grads       NULL: none wanted.  A vector that the call has no use for (w_post without a norm after the block, all but w_pre and
+ *               b_pre without B, w_pre and b_pre without dZ) gets a gradient of 0 where it is wanted
+ *   workspace   pipad_residual_norm_workspace(F, n, k) bytes, or NULL where grads is NULL */
+int pipad_residual_norm_workspace(int32_t F, int32_t n, int32_t k, size_t *bytes);
+int pipad_residual_norm_backward(const pipad_residual_norm_t *norm, int32_t n, int32_t k, const float *const *R, int64_t ldr,
+                                 const float *const *B, int64_t ldb, const float *const *gate, int64_t ldg,
+                                 const float *const *dR_out, int64_t lddro, const float *const *dZ, int64_t lddz,
+                                 float *const *dR, int64_t lddr, float *const *dB, int64_t lddb, float *const *dgate,
+                                 int64_t lddg, const pipad_residual_norm_grads_t *grads, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
+/* The gated feed-forward block:  Y = (act(X Wg + bg) * (X Wu + bu)) Wd + bd
+ * on rows of F columns, through `hidden` columns that stay on the chip, to rows of Fo columns, with weights that all rows share.
+ *   activation  sigmoid, relu, gelu (the exact one, x * Phi(x)) or silu (x * sigmoid(x))
+ *   Wg, Wu      row-major float [F][hidden], row strides ldwg, ldwu >= hidden;  Wd  [hidden][Fo], ldwd >= Fo
+ *   bg, bu, bd  float [hidden], [hidden], [Fo], NULL: none
+ * Widths of 65536 and more are PIPAD_ERR_TOO_LARGE.  Products are exact to the last bits of 32-bit floats (each as six products of
+ * 8-bit pieces, see csrc/pipad_gated_ff.hip); a row with a value that is not finite gives NaN where floats may give an infinity, and no
+ * other row sees it. */
+#define PIPAD_ACT_SIGMOID 0
+#define PIPAD_ACT_RELU 1
+#define PIPAD_ACT_GELU 2
+#define PIPAD_ACT_SILU 3
+typedef struct pipad_gated_ff_params {
+  int32_t F, hidden, Fo, activation;
+  const float *Wg, *Wu, *Wd;
+  int64_t ldwg, ldwu, ldwd;
+  const float *bg, *bu, *bd;
+} pipad_gated_ff_t;
+
+/* Bytes of workspace for a forward (backward = 0) or a backward call (1); only the sizes in `block` are looked at. */
+int pipad_gated_ff_workspace(const pipad_gated_ff_t *block, int32_t n, int32_t k, int32_t backward, size_t *bytes);
+int pipad_gated_ff(const pipad_gated_ff_t *block, int32_t n, int32_t k, const float *const *X, int64_t ldx, float *const *Y,
+                   int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients of weights and biases, each NULL: not wanted; written, not added to.  Shapes as the weights', with their own strides. */
+typedef struct pipad_gated_ff_grads {
+  float *dWg, *dWu, *dWd;
+  int64_t lddwg, lddwu, lddwd;
+  float *dbg, *dbu, *dbd;
+} pipad_gated_ff_grads_t;
+
+/* The gradients of pipad_gated_ff from X and dY: nothing is kept from the forward call, what lies between is made again.
+ *   dX      receives the gradient of X; NULL: not wanted
+ *   grads   NULL: none wanted */
+int pipad_gated_ff_backward(const pipad_gated_ff_t *block, int32_t n, int32_t k, const float *const *X, int64_t ldx,
+                            const float *const *dY, int64_t lddy, float *const *dX, int64_t lddx,
+                            const pipad_gated_ff_grads_t *grads, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Static text for a status code. */
 const char *pipad_strerror(int status);

@@ -6,6 +6,8 @@ this package is the thin binding.  There is no CPU fallback.
 from .binding import (Frame, PipadError, frame_aggregate, frame_aggregate_subset, frame_aggregate_update,
                       frame_build_overlap, frame_transpose, get_option, load_library,
                       set_option)
+from .rows import (GatedFFGrads, ResidualNormGrads, gated_ff, gated_ff_backward, residual_norm,
+                   residual_norm_backward)
 
 
 def coalescent_row_bytes(snapshots: int, feat: int) -> int:
@@ -25,4 +27,5 @@ def padded_row_stride(feat: int) -> int:
 
 
 __all__ = ["Frame", "PipadError", "frame_aggregate", "frame_aggregate_subset", "frame_aggregate_update", "frame_build_overlap", "frame_transpose", "get_option",
-           "set_option", "load_library", "coalescent_row_bytes", "padded_row_stride"]
+           "set_option", "load_library", "GatedFFGrads", "ResidualNormGrads", "gated_ff", "gated_ff_backward", "residual_norm",
+           "residual_norm_backward", "coalescent_row_bytes", "padded_row_stride"]

@@ -71,6 +71,13 @@ SIGNATURES = {
     "pipad_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "pipad_last_hip_error": (ctypes.c_char_p, []),
     "pipad_set_option": (ctypes.c_int, [ctypes.c_char_p, _i64]),
+    # operators on node rows (rows.py)
+    "pipad_residual_norm": (ctypes.c_int, [_vp, _i32, _i32, *[_vp, _i64] * 5, _vp]),
+    "pipad_residual_norm_workspace": (ctypes.c_int, [_i32, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "pipad_residual_norm_backward": (ctypes.c_int, [_vp, _i32, _i32, *[_vp, _i64] * 8, _vp, _vp, ctypes.c_size_t, _vp]),
+    "pipad_gated_ff_workspace": (ctypes.c_int, [_vp, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "pipad_gated_ff": (ctypes.c_int, [_vp, _i32, _i32, *[_vp, _i64] * 2, _vp, ctypes.c_size_t, _vp]),
+    "pipad_gated_ff_backward": (ctypes.c_int, [_vp, _i32, _i32, *[_vp, _i64] * 3, _vp, _vp, ctypes.c_size_t, _vp]),
     # include/pipad_ceilings.h (measurement kernels)
     "pipad_ceiling_stream_read": (ctypes.c_int, [_vp, ctypes.c_size_t, _vp, _vp]),
     "pipad_ceiling_stream_copy": (ctypes.c_int, [_vp, _vp, ctypes.c_size_t, _vp]),

@@ -22,7 +22,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpipad.so")
 SOURCES = ["pipad_api.hip", "pipad_build.hip", "pipad_aggregate.hip", "pipad_transpose.hip",
-           "pipad_ceilings.hip"]
+           "pipad_norm.hip", "pipad_gated_ff.hip", "pipad_ceilings.hip"]
 
 
 def hipcc() -> str:

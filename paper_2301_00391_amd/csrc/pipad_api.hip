@@ -26,6 +26,16 @@ void destroy_frame(pipad_frame *f);
 int transpose_frame(const pipad_frame *f, pipad_alloc_fn alloc, void *alloc_ctx, hipStream_t st,
                     pipad_frame **out);
 
+// k matrices of n rows of F columns: PIPAD_OK, or what is wrong with them.  `at` null where that is allowed is not looked at.
+template <class T>
+static int check_rows(int32_t n, int32_t k, int32_t F, T *const *at, int64_t ld) {
+  if (!at || ld < F) return PIPAD_ERR_INVALID_ARG;
+  if (n > 0)
+    for (int t = 0; t < k; ++t)
+      if (!at[t]) return PIPAD_ERR_INVALID_ARG;
+  return (int64_t)n * ld >= (int64_t)1 << 40 || ld >= (int64_t)1 << 40 ? PIPAD_ERR_TOO_LARGE : PIPAD_OK;
+}
+
 }  // namespace pipad
 
 extern "C" {
@@ -188,6 +198,133 @@ int pipad_frame_transpose(const pipad_frame_t *frame, pipad_alloc_fn alloc, void
   return PIPAD_OK;
 }
 
+// ---- operators on node rows ---------------------------------------------------------------------
+#define PIPAD_ROWS(F, at, ld)                                     \
+  do {                                                            \
+    const int rc__ = pipad::check_rows(n, k, (F), (at), (ld));           \
+    if (rc__ != PIPAD_OK) return rc__;                            \
+  } while (0)
+
+static int check_norm(const pipad_residual_norm_t *c, int32_t n, int32_t k, bool has_b, bool has_gate) {
+  if (!c || n < 0 || k < 1 || k > PIPAD_MAX_K || c->F < 1 || !(c->eps >= 0.f)) return PIPAD_ERR_INVALID_ARG;
+  for (int32_t kind : {c->post, c->pre})
+    if (kind != PIPAD_NORM_NONE && kind != PIPAD_NORM_RMS && kind != PIPAD_NORM_LAYER) return PIPAD_ERR_INVALID_ARG;
+  if (c->post == PIPAD_NORM_NONE && (c->w_post || c->b_post)) return PIPAD_ERR_INVALID_ARG;
+  if (c->pre == PIPAD_NORM_NONE && (c->w_pre || c->b_pre)) return PIPAD_ERR_INVALID_ARG;
+  if (!has_b && (has_gate || c->scale || c->post != PIPAD_NORM_NONE)) return PIPAD_ERR_INVALID_ARG;
+  return c->F > PIPAD_NORM_MAX_F ? PIPAD_ERR_TOO_LARGE : PIPAD_OK;
+}
+
+static int check_workspace(const void *workspace, size_t have, size_t need) {
+  if (need == 0) return PIPAD_OK;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return PIPAD_ERR_INVALID_ARG;
+  return have < need ? PIPAD_ERR_SCRATCH : PIPAD_OK;
+}
+
+int pipad_residual_norm(const pipad_residual_norm_t *norm, int32_t n, int32_t k, const float *const *R, int64_t ldr,
+                        const float *const *B, int64_t ldb, const float *const *gate, int64_t ldg, float *const *R_out,
+                        int64_t ldro, float *const *Z, int64_t ldz, void *stream) {
+  int rc = check_norm(norm, n, k, B != nullptr, gate != nullptr);
+  if (rc != PIPAD_OK) return rc;
+  if ((!R_out && !Z) || (R_out && !B) || (Z && norm->pre == PIPAD_NORM_NONE)) return PIPAD_ERR_INVALID_ARG;
+  PIPAD_ROWS(norm->F, R, ldr);
+  if (B) PIPAD_ROWS(norm->F, B, ldb);
+  if (gate) PIPAD_ROWS(norm->F, gate, ldg);
+  if (R_out) PIPAD_ROWS(norm->F, R_out, ldro);
+  if (Z) PIPAD_ROWS(norm->F, Z, ldz);
+  if (n == 0) return PIPAD_OK;
+  return pipad::residual_norm_launch(*norm, n, k, pipad::NormRows{R, B, gate, nullptr, nullptr, R_out, Z, nullptr, ldr, ldb, ldg, 0, 0, ldro, ldz, 0},
+                                     static_cast<hipStream_t>(stream));
+}
+
+int pipad_residual_norm_workspace(int32_t F, int32_t n, int32_t k, size_t *bytes) {
+  if (!bytes || F < 1 || n < 0 || k < 1 || k > PIPAD_MAX_K) return PIPAD_ERR_INVALID_ARG;
+  if (F > PIPAD_NORM_MAX_F) return PIPAD_ERR_TOO_LARGE;
+  *bytes = pipad::residual_norm_workspace(F, n, k);
+  return PIPAD_OK;
+}
+
+int pipad_residual_norm_backward(const pipad_residual_norm_t *norm, int32_t n, int32_t k, const float *const *R, int64_t ldr,
+                                 const float *const *B, int64_t ldb, const float *const *gate, int64_t ldg,
+                                 const float *const *dR_out, int64_t lddro, const float *const *dZ, int64_t lddz,
+                                 float *const *dR, int64_t lddr, float *const *dB, int64_t lddb, float *const *dgate,
+                                 int64_t lddg, const pipad_residual_norm_grads_t *grads, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+  int rc = check_norm(norm, n, k, B != nullptr, gate != nullptr);
+  if (rc != PIPAD_OK) return rc;
+  if ((!dR_out && !dZ) || (dZ && norm->pre == PIPAD_NORM_NONE) || (dB && !B) || (dgate && !gate) || (!dR && !dB && !dgate && !grads))
+    return PIPAD_ERR_INVALID_ARG;
+  PIPAD_ROWS(norm->F, R, ldr);
+  if (B) PIPAD_ROWS(norm->F, B, ldb);
+  if (gate) PIPAD_ROWS(norm->F, gate, ldg);
+  if (dR_out) PIPAD_ROWS(norm->F, dR_out, lddro);
+  if (dZ) PIPAD_ROWS(norm->F, dZ, lddz);
+  if (dR) PIPAD_ROWS(norm->F, dR, lddr);
+  if (dB) PIPAD_ROWS(norm->F, dB, lddb);
+  if (dgate) PIPAD_ROWS(norm->F, dgate, lddg);
+  float *sums[5] = {};
+  if (grads) {
+    if ((rc = check_workspace(workspace, workspace_bytes, pipad::residual_norm_workspace(norm->F, n, k))) != PIPAD_OK) return rc;
+    sums[0] = grads->dscale, sums[1] = grads->dw_post, sums[2] = grads->db_post, sums[3] = grads->dw_pre, sums[4] = grads->db_pre;
+  }
+  return pipad::residual_norm_backward_launch(*norm, n, k,
+                                              pipad::NormRows{R, B, gate, dR_out, dZ, dR, dB, dgate, ldr, ldb, ldg, lddro, lddz, lddr, lddb, lddg},
+                                              sums, workspace, static_cast<hipStream_t>(stream));
+}
+
+static int check_ff_sizes(const pipad_gated_ff_t *c, int32_t n, int32_t k) {
+  if (!c || n < 0 || k < 1 || k > PIPAD_MAX_K || c->F < 1 || c->hidden < 1 || c->Fo < 1) return PIPAD_ERR_INVALID_ARG;
+  if (c->activation < PIPAD_ACT_SIGMOID || c->activation > PIPAD_ACT_SILU) return PIPAD_ERR_INVALID_ARG;
+  const int32_t lim = 1 << 16;
+  return c->F >= lim || c->hidden >= lim || c->Fo >= lim ? PIPAD_ERR_TOO_LARGE : PIPAD_OK;
+}
+static int check_ff(const pipad_gated_ff_t *c, int32_t n, int32_t k) {
+  const int rc = check_ff_sizes(c, n, k);
+  if (rc != PIPAD_OK) return rc;
+  if (!c->Wg || !c->Wu || !c->Wd || c->ldwg < c->hidden || c->ldwu < c->hidden || c->ldwd < c->Fo) return PIPAD_ERR_INVALID_ARG;
+  const int64_t lim = (int64_t)1 << 40;
+  return c->ldwg >= lim || c->ldwu >= lim || c->ldwd >= lim ? PIPAD_ERR_TOO_LARGE : PIPAD_OK;
+}
+
+int pipad_gated_ff_workspace(const pipad_gated_ff_t *block, int32_t n, int32_t k, int32_t backward, size_t *bytes) {
+  const int rc = check_ff_sizes(block, n, k);
+  if (rc != PIPAD_OK) return rc;
+  if (!bytes || (backward != 0 && backward != 1)) return PIPAD_ERR_INVALID_ARG;
+  *bytes = pipad::gated_ff_workspace(*block, n, k, backward != 0);
+  return PIPAD_OK;
+}
+
+int pipad_gated_ff(const pipad_gated_ff_t *block, int32_t n, int32_t k, const float *const *X, int64_t ldx, float *const *Y,
+                   int64_t ldy, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = check_ff(block, n, k);
+  if (rc != PIPAD_OK) return rc;
+  PIPAD_ROWS(block->F, X, ldx);
+  PIPAD_ROWS(block->Fo, Y, ldy);
+  if (n == 0) return PIPAD_OK;
+  if ((rc = check_workspace(workspace, workspace_bytes, pipad::gated_ff_workspace(*block, n, k, false))) != PIPAD_OK) return rc;
+  return pipad::gated_ff_launch(*block, n, k, X, ldx, Y, ldy, workspace, static_cast<hipStream_t>(stream));
+}
+
+int pipad_gated_ff_backward(const pipad_gated_ff_t *block, int32_t n, int32_t k, const float *const *X, int64_t ldx,
+                            const float *const *dY, int64_t lddy, float *const *dX, int64_t lddx,
+                            const pipad_gated_ff_grads_t *grads, void *workspace, size_t workspace_bytes, void *stream) {
+  int rc = check_ff(block, n, k);
+  if (rc != PIPAD_OK) return rc;
+  PIPAD_ROWS(block->F, X, ldx);
+  PIPAD_ROWS(block->Fo, dY, lddy);
+  if (dX) PIPAD_ROWS(block->F, dX, lddx);
+  if (!dX && !grads) return PIPAD_ERR_INVALID_ARG;
+  if (grads) {
+    const int64_t lim = (int64_t)1 << 40;
+    if ((grads->dWg && grads->lddwg < block->hidden) || (grads->dWu && grads->lddwu < block->hidden) || (grads->dWd && grads->lddwd < block->Fo))
+      return PIPAD_ERR_INVALID_ARG;
+    if ((grads->dWg && grads->lddwg >= lim) || (grads->dWu && grads->lddwu >= lim) || (grads->dWd && grads->lddwd >= lim)) return PIPAD_ERR_TOO_LARGE;
+  }
+  if (n > 0 && (rc = check_workspace(workspace, workspace_bytes, pipad::gated_ff_workspace(*block, n, k, true))) != PIPAD_OK) return rc;
+  return pipad::gated_ff_backward_launch(*block, n, k, X, ldx, dY, lddy, dX, lddx, grads, workspace, static_cast<hipStream_t>(stream));
+}
+#undef PIPAD_ROWS
+
 int64_t pipad_recommended_row_stride(int32_t F) {
   if (F < 1) return PIPAD_ERR_INVALID_ARG;
   if (F <= 32) {  // within one line: the next power of two, so that no row straddles two lines
@@ -219,7 +356,7 @@ const char *pipad_strerror(int status) {
     case PIPAD_ERR_ALLOC: return "device allocation failed";
     case PIPAD_ERR_TOO_LARGE: return "size exceeds the int32 index space";
     case PIPAD_ERR_HIP: return "HIP runtime error";
-    case PIPAD_ERR_SCRATCH: return "the fixed scratch array is too small for this frame and F";
+    case PIPAD_ERR_SCRATCH: return "the fixed scratch array is too small for this frame and F, or a workspace for its call";
     default: return "unknown status";
   }
 }

@@ -391,6 +391,23 @@ int aggregate_launch(const pipad_frame *f, int32_t F, const float *const *X, int
 
 // Address, on the current device, of the library's fixed scratch array (resolved once per device).
 int static_scratch(float **ptr, size_t *floats);
+
+// The operators on node rows (pipad_norm.hip, pipad_gated_ff.hip).  Arguments are checked; a workspace is as large as asked for.
+struct NormRows {  // k matrices each, or null
+  const float *const *R, *const *B, *const *gate, *const *dRout, *const *dZ;
+  float *const *out0, *const *out1, *const *out2;  // R', Z; or dR, dB, dgate
+  int64_t ldr, ldb, ldg, lddro, lddz, ld0, ld1, ld2;
+};
+int residual_norm_launch(const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m, hipStream_t st);
+size_t residual_norm_workspace(int32_t F, int32_t n, int32_t k);
+// sums: where the gradients of scale, w_post, b_post, w_pre, b_pre go, each may be null
+int residual_norm_backward_launch(const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m, float *const (&sums)[5], void *workspace,
+                                  hipStream_t st);
+size_t gated_ff_workspace(const pipad_gated_ff_t &c, int32_t n, int32_t k, bool backward);
+int gated_ff_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float *const *X, int64_t ldx, float *const *Y, int64_t ldy,
+                    void *workspace, hipStream_t st);
+int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float *const *X, int64_t ldx, const float *const *dY,
+                             int64_t lddy, float *const *dX, int64_t lddx, const pipad_gated_ff_grads_t *grads, void *workspace, hipStream_t st);
 }
 
 #endif  // PIPAD_INTERNAL_H_

@@ -1,0 +1,400 @@
+// The norms around a block of a model, fused with its gate and residual scale, and their gradients (pipad_residual_norm,
+// pipad_residual_norm_backward in include/pipad.h).
+//
+//   P = post(B),  R' = R + scale * sigmoid(gate) * P,  Z = pre(R')       post, pre: none, root mean square, or layer norm
+//
+// Everything about a node row is local to the row but the gradients of the vectors that all rows share, so one pass over the
+// matrices does it: a row lies in the registers of LPR lanes, its sums go over these lanes, and nothing is kept from the
+// forward pass but R' itself.  What is read and written once is all that there is to move: 5 matrices forward, 8 backward.
+#include "pipad_internal.h"
+
+namespace pipad {
+
+namespace {
+
+struct NormArgs {
+  const float *R[PIPAD_MAX_K], *B[PIPAD_MAX_K], *gate[PIPAD_MAX_K];      // R: R' in the backward pass
+  const float *dRout[PIPAD_MAX_K], *dZ[PIPAD_MAX_K];                     // backward
+  float *out0[PIPAD_MAX_K], *out1[PIPAD_MAX_K], *out2[PIPAD_MAX_K];      // R', Z; or dR, dB, dgate
+  int64_t ldr, ldb, ldg, lddro, lddz, ld0, ld1, ld2;
+  int32_t n, F, post, pre;
+  float eps, inv_f;
+  const float *scale, *w_post, *b_post, *w_pre, *b_pre;
+  bool has_b, has_gate, has_drout, has_dz, want0, want1, want2;
+  float *partial;  // [block][kSums][F], or null
+};
+
+constexpr int kSums = 5;  // dscale, dw_post, db_post, dw_pre, db_pre
+
+// Sum over the LPR lanes of a row, the same bits in all of them.  256: the whole workgroup, through `lds`, whose turns alternate
+// between two halves so that one barrier a sum is enough.
+template <int LPR>
+__device__ inline float row_sum(float x, float *lds, int &turn) {
+#pragma unroll
+  for (int d = 1; d < (LPR < 64 ? LPR : 64); d <<= 1) x += __shfl_xor(x, d);
+  if (LPR == 256) {
+    float *const at = lds + 4 * turn;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = (at[0] + at[1]) + (at[2] + at[3]);
+  }
+  return x;
+}
+
+__device__ inline float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+
+// The columns of a lane: VEC consecutive ones, NV times, LPR * VEC apart.
+template <int VEC, int LPR, int NV>
+struct Row {
+  static constexpr int kElems = VEC * NV;
+  float v[kElems];
+  __device__ static int column(int lane, int j) { return (j / VEC) * LPR * VEC + lane * VEC + j % VEC; }
+  __device__ void fill(float x) {
+#pragma unroll
+    for (int j = 0; j < kElems; ++j) v[j] = x;
+  }
+  __device__ void load(const float *p, int lane, int F) {
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int c = column(lane, q * VEC);
+      if (VEC == 4) {
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < F) t = *reinterpret_cast<const float4 *>(p + c);
+        v[q * VEC] = t.x, v[q * VEC + 1 % VEC] = t.y, v[q * VEC + 2 % VEC] = t.z, v[q * VEC + 3 % VEC] = t.w;
+      } else {
+        v[q] = c < F ? p[c] : 0.f;
+      }
+    }
+  }
+  __device__ void load_or(const float *p, int lane, int F, float otherwise) {
+    if (p) load(p, lane, F);
+    else fill(otherwise);
+  }
+  __device__ void store(float *p, int lane, int F) const {
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int c = column(lane, q * VEC);
+      if (c < F) {
+        if (VEC == 4) *reinterpret_cast<float4 *>(p + c) = make_float4(v[q * VEC], v[q * VEC + 1 % VEC], v[q * VEC + 2 % VEC], v[q * VEC + 3 % VEC]);
+        else p[c] = v[q];
+      }
+    }
+  }
+};
+
+// x becomes x normalised; columns that are not there stay 0.  Returns the factor.  The layer norm's variance is that of the
+// centred values (a second pass over registers), never a difference of two large sums.
+template <int VEC, int LPR, int NV>
+__device__ inline float normalise(Row<VEC, LPR, NV> &x, int kind, int lane, int F, float inv_f, float eps, float *lds, int &turn) {
+  constexpr int E = VEC * NV;
+  if (kind == PIPAD_NORM_LAYER) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < E; ++j) s += x.v[j];
+    const float mean = row_sum<LPR>(s, lds, turn) * inv_f;
+#pragma unroll
+    for (int j = 0; j < E; ++j) x.v[j] = x.column(lane, j) < F ? x.v[j] - mean : 0.f;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < E; ++j) s = fmaf(x.v[j], x.v[j], s);
+  const float r = rsqrtf(fmaf(row_sum<LPR>(s, lds, turn), inv_f, eps));
+#pragma unroll
+  for (int j = 0; j < E; ++j) x.v[j] *= r;
+  return r;
+}
+
+// d (the gradient of the normalised x) becomes that of what was normalised with factor r.
+template <int VEC, int LPR, int NV>
+__device__ inline void normalise_back(Row<VEC, LPR, NV> &d, const Row<VEC, LPR, NV> &x, float r, int kind, float inv_f, float *lds, int &turn) {
+  constexpr int E = VEC * NV;
+  float s = 0.f, m = 0.f;
+#pragma unroll
+  for (int j = 0; j < E; ++j) s = fmaf(d.v[j], x.v[j], s);
+  s = row_sum<LPR>(s, lds, turn) * inv_f;
+  if (kind == PIPAD_NORM_LAYER) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) m += d.v[j];
+    m = row_sum<LPR>(m, lds, turn) * inv_f;
+  }
+#pragma unroll
+  for (int j = 0; j < E; ++j) d.v[j] = (d.v[j] - m - x.v[j] * s) * r;
+}
+
+template <int VEC, int LPR, int NV>
+__global__ void __launch_bounds__(kBlock) k_residual_norm(NormArgs a) {
+  using R = Row<VEC, LPR, NV>;
+  constexpr int E = R::kElems, kRows = kBlock / LPR;
+  __shared__ float lds[8];
+  int turn = 0;
+  const int lane = threadIdx.x % LPR, t = blockIdx.y, F = a.F;
+  R scale, w_post, b_post, w_pre, b_pre;
+  if (a.has_b) {
+    scale.load_or(a.scale, lane, F, 1.f);
+    w_post.load_or(a.w_post, lane, F, 1.f);
+    b_post.load_or(a.b_post, lane, F, 0.f);
+  }
+  if (a.want1) {
+    w_pre.load_or(a.w_pre, lane, F, 1.f);
+    b_pre.load_or(a.b_pre, lane, F, 0.f);
+  }
+  for (int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR; i < a.n; i += (int64_t)gridDim.x * kRows) {
+    R r, p, gate;
+    r.load(a.R[t] + i * a.ldr, lane, F);
+    if (a.has_b) {
+      p.load(a.B[t] + i * a.ldb, lane, F);
+      if (a.has_gate) gate.load(a.gate[t] + i * a.ldg, lane, F);
+      if (a.post != PIPAD_NORM_NONE) {
+        normalise(p, a.post, lane, F, a.inv_f, a.eps, lds, turn);
+#pragma unroll
+        for (int j = 0; j < E; ++j) p.v[j] = fmaf(p.v[j], w_post.v[j], b_post.v[j]);
+      }
+      if (a.has_gate) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) p.v[j] *= sigmoid_of(gate.v[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < E; ++j) r.v[j] = r.column(lane, j) < F ? fmaf(scale.v[j], p.v[j], r.v[j]) : 0.f;
+      if (a.want0) r.store(a.out0[t] + i * a.ld0, lane, F);
+    }
+    if (a.want1) {
+      normalise(r, a.pre, lane, F, a.inv_f, a.eps, lds, turn);
+#pragma unroll
+      for (int j = 0; j < E; ++j) r.v[j] = fmaf(r.v[j], w_pre.v[j], b_pre.v[j]);
+      r.store(a.out1[t] + i * a.ld1, lane, F);
+    }
+  }
+}
+
+// The sums over all rows: every lane adds up those of its rows, then the workgroup's lanes of one column are added in a fixed
+// order and go to its own place in `partial`; k_norm_sums adds the workgroups.
+template <int VEC, int LPR, int NV>
+__global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
+  using R = Row<VEC, LPR, NV>;
+  constexpr int E = R::kElems, kRows = kBlock / LPR;
+  __shared__ float lds[8];
+  extern __shared__ float sums[];  // [kRows][E * LPR] (more than one row a workgroup)
+  int turn = 0;
+  const int lane = threadIdx.x % LPR, t = blockIdx.y, F = a.F;
+  R scale, w_post, b_post, w_pre, acc[kSums];
+  scale.load_or(a.scale, lane, F, 1.f);
+  w_post.load_or(a.w_post, lane, F, 1.f);
+  b_post.load_or(a.b_post, lane, F, 0.f);
+  w_pre.load_or(a.w_pre, lane, F, 1.f);
+#pragma unroll
+  for (int q = 0; q < kSums; ++q) acc[q].fill(0.f);
+  for (int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR; i < a.n; i += (int64_t)gridDim.x * kRows) {
+    R d, b, gate, g;
+    if (a.has_b) b.load(a.B[t] + i * a.ldb, lane, F);
+    if (a.has_gate) gate.load(a.gate[t] + i * a.ldg, lane, F);
+    if (a.has_drout) g.load(a.dRout[t] + i * a.lddro, lane, F);
+    else g.fill(0.f);
+    if (a.has_dz) {
+      R x;
+      x.load(a.R[t] + i * a.ldr, lane, F);
+      d.load(a.dZ[t] + i * a.lddz, lane, F);
+      const float r = normalise(x, a.pre, lane, F, a.inv_f, a.eps, lds, turn);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        acc[3].v[j] = fmaf(d.v[j], x.v[j], acc[3].v[j]);
+        acc[4].v[j] += d.v[j];
+        d.v[j] *= w_pre.v[j];
+      }
+      normalise_back(d, x, r, a.pre, a.inv_f, lds, turn);
+#pragma unroll
+      for (int j = 0; j < E; ++j) g.v[j] += d.v[j];
+    }
+    if (a.want0) g.store(a.out0[t] + i * a.ld0, lane, F);
+    if (a.has_b) {
+      float r = 1.f;
+      if (a.post != PIPAD_NORM_NONE) r = normalise(b, a.post, lane, F, a.inv_f, a.eps, lds, turn);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const float p = a.post != PIPAD_NORM_NONE ? fmaf(b.v[j], w_post.v[j], b_post.v[j]) : b.v[j];
+        float gs = g.v[j] * scale.v[j];
+        if (a.has_gate) {
+          // (1 - sigmoid) from the same exponential: their difference would lose it where the gate is wide open
+          const float e = __expf(-fabsf(gate.v[j])), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
+          const float sig = gate.v[j] >= 0.f ? big : small;
+          acc[0].v[j] = fmaf(g.v[j], sig * p, acc[0].v[j]);
+          gate.v[j] = gs * p * big * small;
+          gs *= sig;
+        } else {
+          acc[0].v[j] = fmaf(g.v[j], p, acc[0].v[j]);
+        }
+        d.v[j] = gs;
+      }
+      if (a.has_gate && a.want2) gate.store(a.out2[t] + i * a.ld2, lane, F);
+      if (a.post != PIPAD_NORM_NONE) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          acc[1].v[j] = fmaf(d.v[j], b.v[j], acc[1].v[j]);
+          acc[2].v[j] += d.v[j];
+          d.v[j] = d.column(lane, j) < F ? d.v[j] * w_post.v[j] : 0.f;
+        }
+        normalise_back(d, b, r, a.post, a.inv_f, lds, turn);
+      }
+      if (a.want1) d.store(a.out1[t] + i * a.ld1, lane, F);
+    }
+  }
+  if (!a.partial) return;
+  float *const to = a.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kSums * F;
+#pragma unroll
+  for (int q = 0; q < kSums; ++q) {
+    if (LPR == 256) {
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (acc[q].column(lane, j) < F) to[q * F + acc[q].column(lane, j)] = acc[q].v[j];
+      continue;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < E; ++j) sums[(threadIdx.x / LPR) * (E * LPR) + acc[q].column(lane, j)] = acc[q].v[j];
+    __syncthreads();
+    for (int c = threadIdx.x; c < F; c += kBlock) {
+      float s = 0.f;
+      for (int w = 0; w < kRows; ++w) s += sums[w * (E * LPR) + c];
+      to[q * F + c] = s;
+    }
+  }
+}
+
+struct SumOut {
+  float *out[kSums];
+};
+// out[q][c] = the sum of the workgroups' partial[.][q][c], always in the same order: 16 of its lanes take every 16th each.
+__global__ void __launch_bounds__(kBlock) k_norm_sums(const float *partial, int64_t count, int32_t F, SumOut o) {
+  __shared__ float part[16][17];
+  const int x = threadIdx.x % 16, y = threadIdx.x / 16;
+  const int64_t c = (int64_t)blockIdx.x * 16 + x;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (c < (int64_t)kSums * F) {
+    int64_t b = y;
+    for (; b + 48 < count; b += 64) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[u] += partial[(b + 16 * u) * kSums * F + c];
+    }
+    for (; b < count; b += 16) s[0] += partial[b * kSums * F + c];
+  }
+  part[y][x] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (y != 0 || c >= (int64_t)kSums * F) return;
+  float all = 0.f;
+  for (int w = 0; w < 16; ++w) all += part[w][x];
+  const int q = (int)(c / F);
+  if (o.out[q]) o.out[q][c - (int64_t)q * F] = all;
+}
+
+using NormKernel = void (*)(NormArgs);
+struct NormPlan {
+  NormKernel forward, backward;
+  int lanes, elems;  // of a row: LPR, VEC * NV
+};
+
+template <int VEC, int LPR, int NV>
+NormPlan plan_of() {
+  return {k_residual_norm<VEC, LPR, NV>, k_residual_norm_backward<VEC, LPR, NV>, LPR, VEC * NV};
+}
+
+// The fewest lanes that hold a row with one load each, up to a wave; then up to four (16 single) columns a lane more, then the
+// whole workgroup.  `vec`: every row starts on 16 bytes and is a multiple of 4 long.
+NormPlan plan(int32_t F, bool vec) {
+  if (vec) {
+    if (F <= 4) return plan_of<4, 1, 1>();
+    if (F <= 8) return plan_of<4, 2, 1>();
+    if (F <= 16) return plan_of<4, 4, 1>();
+    if (F <= 32) return plan_of<4, 8, 1>();
+    if (F <= 64) return plan_of<4, 16, 1>();
+    if (F <= 128) return plan_of<4, 32, 1>();
+    if (F <= 256) return plan_of<4, 64, 1>();
+    if (F <= 512) return plan_of<4, 64, 2>();
+    if (F <= 1024) return plan_of<4, 64, 4>();
+    return plan_of<4, 256, 4>();
+  }
+  if (F <= 1) return plan_of<1, 1, 1>();
+  if (F <= 2) return plan_of<1, 2, 1>();
+  if (F <= 4) return plan_of<1, 4, 1>();
+  if (F <= 8) return plan_of<1, 8, 1>();
+  if (F <= 16) return plan_of<1, 16, 1>();
+  if (F <= 32) return plan_of<1, 32, 1>();
+  if (F <= 64) return plan_of<1, 64, 1>();
+  if (F <= 128) return plan_of<1, 64, 2>();
+  if (F <= 256) return plan_of<1, 64, 4>();
+  if (F <= 512) return plan_of<1, 64, 8>();
+  if (F <= 1024) return plan_of<1, 64, 16>();
+  return plan_of<1, 256, 16>();
+}
+
+// Workgroups a snapshot: rows for all of them, at most about 8 a compute unit over all snapshots.
+constexpr int kMostGroups = 2048;
+int64_t groups(int32_t n, int32_t k, int lanes) {
+  const int64_t rows = kBlock / lanes, all = ((int64_t)n + rows - 1) / rows;
+  return std::max<int64_t>(1, std::min<int64_t>(all, (kMostGroups + k - 1) / k));
+}
+
+bool aligned(const float *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 4 == 0; }
+
+}  // namespace
+
+size_t residual_norm_workspace(int32_t F, int32_t n, int32_t k) {
+  if (n == 0) return 0;
+  // (the rows' alignment is not known here: the most workgroups that any layout takes)
+  return (size_t)groups(n, k, 256) * k * kSums * F * sizeof(float);
+}
+
+static int fill(NormArgs *a, const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m) {
+  a->n = n, a->F = c.F, a->post = c.post, a->pre = c.pre, a->eps = c.eps, a->inv_f = 1.f / (float)c.F;
+  a->scale = c.scale, a->w_post = c.w_post, a->b_post = c.b_post, a->w_pre = c.w_pre, a->b_pre = c.b_pre;
+  a->has_b = m.B != nullptr, a->has_gate = m.gate != nullptr, a->has_drout = m.dRout != nullptr, a->has_dz = m.dZ != nullptr;
+  a->want0 = m.out0 != nullptr, a->want1 = m.out1 != nullptr, a->want2 = m.out2 != nullptr;
+  a->ldr = m.ldr, a->ldb = m.ldb, a->ldg = m.ldg, a->lddro = m.lddro, a->lddz = m.lddz, a->ld0 = m.ld0, a->ld1 = m.ld1, a->ld2 = m.ld2;
+  bool vec = c.F % 4 == 0;
+  for (const float *v : {c.scale, c.w_post, c.b_post, c.w_pre, c.b_pre}) vec = vec && aligned(v, 0);
+  const auto take = [&](auto *const *from, auto *to, int64_t ld) {
+    for (int t = 0; from && t < k; ++t) {
+      to[t] = from[t];
+      vec = vec && aligned(from[t], ld);
+    }
+  };
+  take(m.R, a->R, m.ldr), take(m.B, a->B, m.ldb), take(m.gate, a->gate, m.ldg), take(m.dRout, a->dRout, m.lddro), take(m.dZ, a->dZ, m.lddz);
+  take(m.out0, a->out0, m.ld0), take(m.out1, a->out1, m.ld1), take(m.out2, a->out2, m.ld2);
+  return vec;
+}
+
+int residual_norm_launch(const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m, hipStream_t st) {
+  NormArgs a{};
+  const NormPlan p = plan(c.F, fill(&a, c, n, k, m));
+  hipLaunchKernelGGL(p.forward, dim3((unsigned)groups(n, k, p.lanes), (unsigned)k), dim3(kBlock), 0, st, a);
+  PIPAD_HIP(hipGetLastError());
+  return PIPAD_OK;
+}
+
+int residual_norm_backward_launch(const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m, float *const (&sums)[5], void *workspace,
+                                  hipStream_t st) {
+  bool any = false;
+  SumOut o{};
+  for (int q = 0; q < kSums; ++q) {
+    o.out[q] = sums[q];
+    any = any || sums[q];
+  }
+  int64_t count = 0;
+  if (n > 0) {
+    NormArgs a{};
+    const NormPlan p = plan(c.F, fill(&a, c, n, k, m));
+    const int64_t g = groups(n, k, p.lanes);
+    a.partial = any ? static_cast<float *>(workspace) : nullptr;
+    count = g * k;
+    const size_t lds = any && p.lanes < kBlock ? (size_t)kBlock * p.elems * sizeof(float) : 0;
+    hipLaunchKernelGGL(p.backward, dim3((unsigned)g, (unsigned)k), dim3(kBlock), lds, st, a);
+    PIPAD_HIP(hipGetLastError());
+  }
+  if (any) {
+    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((kSums * (int64_t)c.F + 15) / 16)), dim3(kBlock), 0, st,
+                       static_cast<const float *>(workspace), count, c.F, o);
+    PIPAD_HIP(hipGetLastError());
+  }
+  return PIPAD_OK;
+}
+
+}  // namespace pipad
