@@ -33,6 +33,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32, kDepth = 16;
 constexpr int kFragment = 3 * kWave;  // the three pieces of a 32 x 16 operand, in 16-byte words
+__host__ __device__ constexpr int gu_words(int fq) { return fq * 2 * kFragment + kWave; }  // of a hidden tile
 
 __host__ __device__ constexpr int64_t tiles(int64_t x, int64_t t) { return (x + t - 1) / t; }
 
@@ -138,10 +139,11 @@ struct FfArgs {
   int32_t n, F, hidden, Fo;
   int32_t ht, fq, oq, ft, ot;  // 32-column tiles of the hidden columns, 16- and 32-column tiles of X's and Y's
   bool vec_x, vec_dy, vec_o;
-  // Weights as fragments.  gu: [ht][fq][Wg, Wu], m = hidden column, depth = X's columns.  down: [ht][ot][2], m = Y's column, depth of a
+  // Weights as fragments.  gu: [ht], each [fq][Wg, Wu], m = hidden column, depth = X's columns, and behind them the biases of the tile's
+  // hidden columns (32 floats of bg, 32 of bu, 256 bytes unused), 0 where there are none.  down: [ht][ot][2], m = Y's column, depth of a
   // result = hidden.  up: [ht][oq], m = hidden, depth = Y's columns (Wd).  back: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
   const u32x4 *gu, *down, *up, *back;
-  const float *bg, *bu, *bd;  // padded with zeros to whole tiles
+  const float *bd;  // padded with zeros to whole tiles
   // weight gradients: partial sums of `parts` ranges of rows, each [dWg F x hidden | dWu | dWd hidden x Fo | dbg | dbu | dbd]
   float *partial;
   int64_t part_floats, tiles_per_part;
@@ -219,18 +221,13 @@ struct PackArgs {
   int32_t F, hidden, Fo, ht, fq, oq, ft, ot;
   int64_t n_gu, n_down, n_up, n_back;  // fragments of each kind (0: not wanted)
   u32x4 *gu, *down, *up, *back;
-  float *pbg, *pbu, *pbd;
+  float *pbd;
 };
 __global__ void __launch_bounds__(kBlock) k_ff_pack(PackArgs a) {
   const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
   int64_t at = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kWave;
-  if (at == 0) {  // the biases, by the first wave
-    for (int c = lane; c < a.ht * kTile; c += kWave) {
-      a.pbg[c] = a.bg && c < a.hidden ? a.bg[c] : 0.f;
-      a.pbu[c] = a.bu && c < a.hidden ? a.bu[c] : 0.f;
-    }
+  if (at == 0)  // the last bias, by the first wave
     for (int c = lane; c < a.ot * kTile; c += kWave) a.pbd[c] = a.bd && c < a.Fo ? a.bd[c] : 0.f;
-  }
   float v[8];
   u32x4 *to;
   if (at < a.n_gu) {
@@ -243,7 +240,11 @@ __global__ void __launch_bounds__(kBlock) k_ff_pack(PackArgs a) {
       const int f = q * kDepth + 8 * g + j;
       v[j] = f < a.F && hid < a.hidden ? W[f * ld + hid] : 0.f;
     }
-    to = a.gu + at * kFragment;
+    to = a.gu + (int64_t)h * gu_words(a.fq) + (at - (int64_t)h * a.fq * 2) * kFragment;
+    if (at == (int64_t)h * a.fq * 2) {  // the tile's biases, by the wave of its first fragment
+      const float *const b = g ? a.bu : a.bg;
+      reinterpret_cast<float *>(a.gu + (int64_t)h * gu_words(a.fq) + a.fq * 2 * kFragment)[lane] = b && hid < a.hidden ? b[hid] : 0.f;
+    }
   } else if ((at -= a.n_gu) < a.n_down) {
     const int s = (int)(at % 2), o = (int)(at / 2 % a.ot), h = (int)(at / 2 / a.ot), fo = o * kTile + m;
 #pragma unroll
@@ -292,14 +293,15 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
 #pragma unroll
   for (int o = 0; o < OT; ++o) y[o] = o0 + o < a.ot ? per_row(a.bd + (o0 + o) * kTile, g) : zeros();
   for (int h = 0; h < a.ht; ++h) {
-    f32x16 G = per_row(a.bg + h * kTile, g), U = per_row(a.bu + h * kTile, g);
+    const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
+    const float *const bias = reinterpret_cast<const float *>(gu + a.fq * 2 * kFragment);
+    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g);
     for (int q = 0; q < a.fq; ++q) {
       float v[8];
       load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
       const Split b = split8(v);
-      const int64_t w = ((int64_t)h * a.fq + q) * 2;
-      G = product(fragment(a.gu, w), b, G);
-      U = product(fragment(a.gu, w + 1), b, U);
+      G = product(fragment(gu, 2 * q), b, G);
+      U = product(fragment(gu, 2 * q + 1), b, U);
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
@@ -317,6 +319,70 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
   for (int o = 0; o < OT; ++o) store_tile(y[o], out, (o0 + o) * kTile, a.Fo, a.vec_o, g);
 }
 
+// The same where a row's columns, and those of its result, are 128 at most: X's pieces stay in registers, and the waves of a workgroup, 32 node
+// rows each, share the weights through LDS.  A hidden tile's weights come in two phases, [Wg, Wu, biases] and [Wd], each into a buffer of its
+// own while the other is multiplied: loaded past the registers, one barrier a phase.  What is in flight is waited for before the barrier.
+template <int WAVES, int WORDS>
+__device__ inline void stage(const u32x4 *from, u32x4 *to) {
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kWave;
+#pragma unroll
+  for (int i = 0; i < WORDS; i += WAVES * kWave)
+    if (i + WAVES * kWave <= WORDS || i + wave < WORDS)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(from + i + wave + lane),
+                                       (__attribute__((address_space(3))) void *)(to + i + wave), 16, 0, 0);
+}
+__device__ inline void staged() {
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  __syncthreads();
+}
+
+template <int ACT, int FQ, int OT, int WAVES>
+__global__ void __launch_bounds__(WAVES *kWave, 2) k_ff_kept(FfArgs a) {
+  constexpr int kGu = gu_words(FQ), kDown = OT * 2 * kFragment;
+  __shared__ u32x4 gu[kGu], down[kDown];  // (two arrays: what is read of one does not wait for what is loaded into the other)
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
+  const int64_t base = ((int64_t)blockIdx.x * WAVES + threadIdx.x / kWave) * kTile;
+  stage<WAVES, kGu>(a.gu, gu);
+  const RowAt at = row_at(a, base < a.rows ? base : a.rows - 1, m);
+  Split x[FQ];
+  {
+    const float *const row = a.X[at.t] + at.i * a.ldx;
+    float v[FQ][8];
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) load8(v[q], row, q * kDepth + 8 * g, a.F, a.vec_x);
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) x[q] = split8(v[q]);
+  }
+  f32x16 y[OT];
+#pragma unroll
+  for (int o = 0; o < OT; ++o) y[o] = per_row(a.bd + o * kTile, g);
+  const float *const bias = reinterpret_cast<const float *>(gu + FQ * 2 * kFragment);
+  for (int h = 0; h < a.ht; ++h) {
+    staged();
+    stage<WAVES, kDown>(a.down + (int64_t)h * kDown, down);
+    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g);
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) {
+      G = product(fragment(gu, 2 * q), x[q], G);
+      U = product(fragment(gu, 2 * q + 1), x[q], U);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
+    staged();
+    if (h + 1 < a.ht) stage<WAVES, kGu>(a.gu + (int64_t)(h + 1) * kGu, gu);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const Split b = half(G, s);
+#pragma unroll
+      for (int o = 0; o < OT; ++o) y[o] = product(fragment(down, 2 * o + s), b, y[o]);
+    }
+  }
+  if (base + m >= a.rows) return;
+  float *const out = a.out[at.t] + at.i * a.ldo;
+#pragma unroll
+  for (int o = 0; o < OT; ++o) store_tile(y[o], out, o * kTile, a.Fo, a.vec_o, g);
+}
+
 // ---- the gradient of X --------------------------------------------------------------------------
 template <int ACT, int FT>
 __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
@@ -330,14 +396,15 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
 #pragma unroll
   for (int f = 0; f < FT; ++f) dx[f] = zeros();
   for (int h = 0; h < a.ht; ++h) {
-    f32x16 G = per_row(a.bg + h * kTile, g), U = per_row(a.bu + h * kTile, g), dH = zeros();
+    const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
+    const float *const bias = reinterpret_cast<const float *>(gu + a.fq * 2 * kFragment);
+    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g), dH = zeros();
     float v[8];
     for (int q = 0; q < a.fq; ++q) {
       load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
       const Split b = split8(v);
-      const int64_t w = ((int64_t)h * a.fq + q) * 2;
-      G = product(fragment(a.gu, w), b, G);
-      U = product(fragment(a.gu, w + 1), b, U);
+      G = product(fragment(gu, 2 * q), b, G);
+      U = product(fragment(gu, 2 * q + 1), b, U);
     }
     for (int q = 0; q < a.oq; ++q) {
       load8(v, dy, q * kDepth + 8 * g, a.Fo, a.vec_dy);
@@ -380,7 +447,9 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
 #pragma unroll
   for (int t = 0; t < T; ++t) dwg[t] = dwu[t] = dwd[t] = zeros();
   float dbg = 0.f, dbu = 0.f, dbd[T] = {};
-  const float bg = a.bg[h * kTile + m], bu = a.bu[h * kTile + m];
+  const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
+  const float *const bias = reinterpret_cast<const float *>(gu + a.fq * 2 * kFragment);
+  const float bg = bias[m], bu = bias[kTile + m];
   const int64_t first = blockIdx.y * a.tiles_per_part * kTile;
   const int64_t end = first + a.tiles_per_part * kTile < a.rows ? first + a.tiles_per_part * kTile : a.rows;
   for (int64_t base = first; base < end; base += kTile) {
@@ -395,9 +464,8 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
     for (int q = 0; q < a.fq; ++q) {
       load8(v, x, q * kDepth + 8 * g, there ? a.F : 0, a.vec_x);
       const Split b = split8(v, sign);
-      const int64_t w = ((int64_t)h * a.fq + q) * 2;
-      G = product(b, fragment(a.gu, w), G);
-      U = product(b, fragment(a.gu, w + 1), U);
+      G = product(b, fragment(gu, 2 * q), G);
+      U = product(b, fragment(gu, 2 * q + 1), U);
     }
     for (int q = 0; q < a.oq; ++q) {
       load8(v, dy, q * kDepth + 8 * g, there ? a.Fo : 0, a.vec_dy);
@@ -527,16 +595,26 @@ __global__ void __launch_bounds__(kBlock) k_ff_sums(SumArgs a) {
 // ---- host ---------------------------------------------------------------------------------------
 bool aligned(const float *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 4 == 0; }
 
+// Tiles of up to 128 columns: as many as one of the kernels that keep a row has; behind the columns that there are the fragments hold 0.
+constexpr int kKept = 128;
+int32_t column_tiles(int32_t F) {
+  const int32_t t = (int32_t)tiles(F, kTile);
+  return F > kKept || t <= 2 ? t : 4;
+}
+int32_t depth_tiles(int32_t F) {
+  const int32_t t = (int32_t)tiles(F, kDepth);
+  return F > kKept || t <= 2 ? t : t <= 4 ? 4 : t <= 6 ? 6 : 8;
+}
+
 // What lies where in the workspace (bytes), the same for the size query and the calls.
 struct Plan {
   int32_t ht, fq, oq, ft, ot;
   int64_t n_gu, n_down, n_up, n_back;
-  size_t gu, down, up, back, bg, bu, bd, partial, total;
+  size_t gu, down, up, back, bd, partial, total;
   int64_t rows, part_floats, parts, tiles_per_part;
   Plan(const pipad_gated_ff_t &c, int32_t n, int32_t k, bool backward) {
     ht = (int32_t)tiles(c.hidden, kTile);
-    fq = (int32_t)tiles(c.F, kDepth), ft = (int32_t)tiles(c.F, kTile);
-    oq = (int32_t)tiles(c.Fo, kDepth), ot = (int32_t)tiles(c.Fo, kTile);
+    fq = depth_tiles(c.F), ft = column_tiles(c.F), oq = depth_tiles(c.Fo), ot = column_tiles(c.Fo);
     n_gu = (int64_t)ht * fq * 2;
     n_down = backward ? 0 : (int64_t)ht * ot * 2;
     n_up = backward ? (int64_t)ht * oq : 0;
@@ -548,9 +626,9 @@ struct Plan {
       return here;
     };
     const size_t fragment_bytes = kFragment * sizeof(u32x4);
-    gu = take(n_gu * fragment_bytes), down = take(n_down * fragment_bytes);
+    gu = take((size_t)ht * gu_words(fq) * sizeof(u32x4)), down = take(n_down * fragment_bytes);
     up = take(n_up * fragment_bytes), back = take(n_back * fragment_bytes);
-    bg = take(ht * kTile * sizeof(float)), bu = take(ht * kTile * sizeof(float)), bd = take(ot * kTile * sizeof(float));
+    bd = take(ot * kTile * sizeof(float));
     // about two waves a SIMD for the weights' gradients, and four tiles of rows at least for each
     rows = (int64_t)n * k;
     part_floats = 2 * (int64_t)c.F * c.hidden + (int64_t)c.hidden * c.Fo + 2 * (int64_t)c.hidden + c.Fo;
@@ -577,7 +655,6 @@ FfArgs arguments(const pipad_gated_ff_t &c, const Plan &p, int32_t n, int32_t k,
   a.ht = p.ht, a.fq = p.fq, a.oq = p.oq, a.ft = p.ft, a.ot = p.ot;
   a.gu = reinterpret_cast<const u32x4 *>(ws + p.gu), a.down = reinterpret_cast<const u32x4 *>(ws + p.down);
   a.up = reinterpret_cast<const u32x4 *>(ws + p.up), a.back = reinterpret_cast<const u32x4 *>(ws + p.back);
-  a.bg = reinterpret_cast<const float *>(ws + p.bg), a.bu = reinterpret_cast<const float *>(ws + p.bu);
   a.bd = reinterpret_cast<const float *>(ws + p.bd);
   a.partial = reinterpret_cast<float *>(ws + p.partial), a.part_floats = p.part_floats, a.tiles_per_part = p.tiles_per_part;
   return a;
@@ -589,8 +666,7 @@ int pack(const pipad_gated_ff_t &c, const Plan &p, char *ws, hipStream_t st) {
              c.hidden, c.Fo, p.ht,     p.fq,   p.oq,
              p.ft,   p.ot,   p.n_gu,   p.n_down, p.n_up,
              p.n_back, reinterpret_cast<u32x4 *>(ws + p.gu), reinterpret_cast<u32x4 *>(ws + p.down), reinterpret_cast<u32x4 *>(ws + p.up),
-             reinterpret_cast<u32x4 *>(ws + p.back), reinterpret_cast<float *>(ws + p.bg), reinterpret_cast<float *>(ws + p.bu),
-             reinterpret_cast<float *>(ws + p.bd)};
+             reinterpret_cast<u32x4 *>(ws + p.back), reinterpret_cast<float *>(ws + p.bd)};
   const int64_t waves = p.n_gu + p.n_down + p.n_up + p.n_back;
   hipLaunchKernelGGL(k_ff_pack, dim3((unsigned)tiles(waves, kWavesPerBlock)), dim3(kBlock), 0, st, a);
   PIPAD_HIP(hipGetLastError());
@@ -609,6 +685,38 @@ PIPAD_FF_KERNELS(k_ff_rows_backward)
 PIPAD_FF_KERNELS(k_ff_weights_backward)
 #undef PIPAD_FF_KERNELS
 
+struct Kept {
+  void (*kernel)(FfArgs);
+  int waves;
+};
+template <int ACT, int FQ, int OT>
+Kept kept_of() {
+  constexpr int kWaves = FQ <= 4 && OT <= 2 ? 4 : 8;
+  return {k_ff_kept<ACT, FQ, OT, kWaves>, kWaves};
+}
+template <int ACT, int FQ>
+Kept kept_of(int ot) {
+  return ot == 1 ? kept_of<ACT, FQ, 1>() : ot == 2 ? kept_of<ACT, FQ, 2>() : kept_of<ACT, FQ, 4>();
+}
+template <int ACT>
+Kept kept_of(int fq, int ot) {
+  switch (fq) {
+    case 1: return kept_of<ACT, 1>(ot);
+    case 2: return kept_of<ACT, 2>(ot);
+    case 4: return kept_of<ACT, 4>(ot);
+    case 6: return kept_of<ACT, 6>(ot);
+    default: return kept_of<ACT, 8>(ot);
+  }
+}
+Kept kept(int act, int fq, int ot) {
+  switch (act) {
+    case PIPAD_ACT_SIGMOID: return kept_of<PIPAD_ACT_SIGMOID>(fq, ot);
+    case PIPAD_ACT_RELU: return kept_of<PIPAD_ACT_RELU>(fq, ot);
+    case PIPAD_ACT_GELU: return kept_of<PIPAD_ACT_GELU>(fq, ot);
+    default: return kept_of<PIPAD_ACT_SILU>(fq, ot);
+  }
+}
+
 int width(int t) { return t <= 1 ? 0 : t <= 2 ? 1 : 2; }  // which of 1, 2, 4 tiles
 
 }  // namespace
@@ -622,6 +730,12 @@ int gated_ff_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float
   const int rc = pack(c, p, ws, st);
   if (rc != PIPAD_OK) return rc;
   const FfArgs a = arguments(c, p, n, k, X, ldx, nullptr, 0, Y, ldy, ws);
+  if (c.F <= kKept && c.Fo <= kKept) {
+    const Kept f = kept(c.activation, p.fq, p.ot);
+    hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, kTile * f.waves)), dim3(f.waves * kWave), 0, st, a);
+    PIPAD_HIP(hipGetLastError());
+    return PIPAD_OK;
+  }
   const int w = width(p.ot);
   hipLaunchKernelGGL(k_ff_rows_of[c.activation][w], dim3((unsigned)tiles(p.rows, kTile * kWavesPerBlock), (unsigned)tiles(p.ot, 1 << w)),
                      dim3(kBlock), 0, st, a);
