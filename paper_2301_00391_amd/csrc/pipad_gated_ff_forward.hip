@@ -1,0 +1,90 @@
+// The gated feed-forward block, forward, on rows of up to 128 columns.
+#include "pipad_gated_ff.h"
+
+namespace pipad {
+namespace ff {
+
+namespace {
+
+// The same where a row's columns, and those of its result, are 128 at most: X's pieces stay in registers, and the waves of a workgroup, 32 node
+// rows each, share the weights through LDS.  A hidden tile's weights come in two phases, [Wg, Wu, biases] and [Wd], each into a buffer of its
+// own while the other is multiplied: loaded past the registers, one barrier a phase.  What is in flight is waited for before the barrier.
+template <int ACT, int FQ, int OT, int WAVES>
+__global__ void __launch_bounds__(WAVES *kWave, 2) k_ff_kept(FfArgs a) {
+  constexpr int kGu = gu_words(FQ), kDown = OT * 2 * kFragment;
+  __shared__ u32x4 gu[kGu], down[kDown];  // (two arrays: what is read of one does not wait for what is loaded into the other)
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
+  const int64_t base = ((int64_t)blockIdx.x * WAVES + threadIdx.x / kWave) * kTile;
+  stage<WAVES, kGu>(a.gu, gu);
+  const RowAt at = row_at(a, base < a.rows ? base : a.rows - 1, m);
+  Split x[FQ];
+  {
+    const float *const row = a.X[at.t] + at.i * a.ldx;
+    float v[FQ][8];
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) load8(v[q], row, q * kDepth + 8 * g, a.F, a.vec_x);
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) x[q] = split8(v[q]);
+  }
+  f32x16 y[OT];
+#pragma unroll
+  for (int o = 0; o < OT; ++o) y[o] = per_row(a.bd + o * kTile, g);
+  const float *const bias = reinterpret_cast<const float *>(gu + FQ * 2 * kFragment);
+  for (int h = 0; h < a.ht; ++h) {
+    staged();
+    stage<WAVES, kDown>(a.down + (int64_t)h * kDown, down);
+    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g);
+#pragma unroll
+    for (int q = 0; q < FQ; ++q) {
+      G = product(fragment(gu, 2 * q), x[q], G);
+      U = product(fragment(gu, 2 * q + 1), x[q], U);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
+    staged();
+    if (h + 1 < a.ht) stage<WAVES, kGu>(a.gu + (int64_t)(h + 1) * kGu, gu);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const Split b = half(G, s);
+#pragma unroll
+      for (int o = 0; o < OT; ++o) y[o] = product(fragment(down, 2 * o + s), b, y[o]);
+    }
+  }
+  if (base + m >= a.rows) return;
+  float *const out = a.out[at.t] + at.i * a.ldo;
+#pragma unroll
+  for (int o = 0; o < OT; ++o) store_tile(y[o], out, o * kTile, a.Fo, a.vec_o, g);
+}
+
+template <int ACT, int FQ, int OT>
+Kept kept_of() {
+  constexpr int kWaves = FQ <= 4 && OT <= 2 ? 4 : 8;
+  return {k_ff_kept<ACT, FQ, OT, kWaves>, kWaves};
+}
+template <int ACT, int FQ>
+Kept kept_of(int ot) {
+  return ot == 1 ? kept_of<ACT, FQ, 1>() : ot == 2 ? kept_of<ACT, FQ, 2>() : kept_of<ACT, FQ, 4>();
+}
+template <int ACT>
+Kept kept_of(int fq, int ot) {
+  switch (fq) {
+    case 1: return kept_of<ACT, 1>(ot);
+    case 2: return kept_of<ACT, 2>(ot);
+    case 4: return kept_of<ACT, 4>(ot);
+    case 6: return kept_of<ACT, 6>(ot);
+    default: return kept_of<ACT, 8>(ot);
+  }
+}
+}  // namespace
+
+Kept kept_forward(int act, int fq, int ot) {
+  switch (act) {
+    case PIPAD_ACT_SIGMOID: return kept_of<PIPAD_ACT_SIGMOID>(fq, ot);
+    case PIPAD_ACT_RELU: return kept_of<PIPAD_ACT_RELU>(fq, ot);
+    case PIPAD_ACT_GELU: return kept_of<PIPAD_ACT_GELU>(fq, ot);
+    default: return kept_of<PIPAD_ACT_SILU>(fq, ot);
+  }
+}
+
+}  // namespace ff
+}  // namespace pipad
