@@ -1,4 +1,4 @@
-// The gated feed-forward block on node rows, and its gradients (pipad_gated_ff, pipad_gated_ff_backward in include/pipad.h).
+// The gated feed-forward block on node rows, and its gradients (pipad_gated_ff, pipad_gated_ff_backward in include/pipad.h): what its kernels share.
 //
 //   G = X Wg + bg,  U = X Wu + bu,  H = act(G) * U,  Y = H Wd + bd
 //
@@ -6,15 +6,24 @@
 // a time, and its share of H goes from the registers where the matrix instructions left it straight into the next product.  The
 // backward pass makes G and U again, which is two products out of eleven, where keeping them would be 8 bytes a hidden column and row.
 //
-// Products of 32-bit floats from matrix instructions on bf16: x = x1 + x2 + x3, each piece the nearest with 8 bits to what is left, so
-// that the sum has all 24 bits of x.  Of the nine products of pieces the three smallest are left out: x2 y3 and x3 y2 are below 2^-8 2^-17 of
-// the whole each, with either sign.  Six instructions of 32 cycles for 32 x 32 x 16 are 2.7 times as fast as the matrix instructions on floats.
-// A value that is not finite (or above 3.389e38, which rounds to none that is) has no such pieces: its row's results are NaN where floats would
-// give an infinity.
+// Products of 32-bit floats from matrix instructions on 16-bit ones: x s = h1 + h2, each piece the nearest with 11 bits to what is left; h1 k1 +
+// h1 k2 + h2 k1, the fourth product being below 2^-22 of the whole, summed in 32 bits.  Pieces hold 22 bits and a sign, so an operand is off by
+// 2^-22 at most and 2^-24 on average; the error of a sum of 64 products came out as 1.0e-7 of its size (1.4e-7 for a chain of 32-bit
+// multiply-adds, whose roundings are more).  Three instructions of 32 cycles for 32 x 32 x 16 are 5.3 times as fast as the matrix instructions on
+// floats; bf16 pieces hold the last two bits, too, but take three each and six products, and the card's power is what bounds these
+// kernels: 8 million rows of 64 through 171 columns took 2.85 ms with them.
 //
-// The sums are 32-bit floats.  An instruction aligns what it adds to the largest of it and cuts off, so a sum comes out low by some 8e-9
-// of its terms' size; over millions of rows that would be seen, and the weights' gradients are taken with every other tile of rows negated,
-// where it comes out high.  Over 1024 terms of one sign accumulated by the instructions alone it was 4e-7; the gradients' sums are therefore made
+// A 16-bit float reaches from 2^-24 to 2^16, so operands are scaled, by powers of two: rows of X and dY by their largest value, weights by the
+// largest of the block that goes with 32 hidden columns, H, dG and dU by the largest of a node's (or in the weights' gradients a hidden column's)
+// 32 values at a time, whose products are added up outside.  Largest values come to 2^14 .. 2^15.  Two forms:
+//  - wide, for X, dY and their partners forward and in the gradient of X: h2 is kept 2^11 larger and its products are summed apart, so that
+//    values down to 2^-29 of the largest have all their bits, and smaller ones an error of 2^-51 of it;
+//  - narrow, for H, dG and dU in the products with weights, and in the weights' gradients throughout, which the additions to two sums bound:
+//    h2 as it is, one sum; all bits down to 2^-18 of the largest, an error of 2^-40 of it below.
+// A value that is not finite makes its row NaN (or infinite).
+//
+// An instruction aligns what it adds to the largest of it and cuts off, so a sum comes out low by some 1e-8 of its terms' size; over millions of
+// rows that would be seen, and the weights' gradients are taken with every other tile of rows negated, where it comes out high.  They are sums
 // of sums of 32 rows by additions that round to the nearest.
 //
 // How a 32 x 32 x 16 instruction lies in a wave, m = lane % 32, g = lane / 32: the left operand's lane holds row m, the right one's
@@ -29,108 +38,179 @@
 namespace pipad {
 namespace ff {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32, kDepth = 16;
-constexpr int kFragment = 3 * kWave;  // the three pieces of a 32 x 16 operand, in 16-byte words
-__host__ __device__ constexpr int gu_words(int fq) { return fq * 2 * kFragment + kWave; }  // of a hidden tile
+constexpr int kFragment = 2 * kWave;  // the two pieces of a 32 x 16 operand, in 16-byte words
+constexpr float kWide = 2048.f;       // what h2 is multiplied by in the wide form
+// Wg's and Wu's fragments of a hidden tile, and its vectors behind them (struct TileVectors).
+__host__ __device__ constexpr int gu_words(int fq) { return fq * 2 * kFragment + kWave; }
+struct TileVectors {
+  float bg[kTile], bu[kTile];
+  float inv_gu, inv_up, inv_down, inv_back;  // 1 over the scales of the tile's weights
+};
+static_assert(sizeof(TileVectors) <= kWave * sizeof(u32x4), "fits behind the fragments");
 
 __host__ __device__ constexpr int64_t tiles(int64_t x, int64_t t) { return (x + t - 1) / t; }
 
 __device__ inline int result_depth(int s, int g, int j) { return 16 * s + 8 * (j / 4) + 4 * g + j % 4; }
 
-struct Split {
-  u32x4 p[3];
+// ---- scales and pieces --------------------------------------------------------------------------
+struct Scale {
+  float to, inv;  // powers of two, 1 / to
 };
-__device__ inline Split split8(const float (&v)[8]) {
+// Brings the largest magnitude to 2^14 .. 2^15; below 2^-100, and for 0, by 2^114 all the same, so that both factors are ordinary floats.
+__device__ inline Scale scale_for(float largest) {
+  const uint32_t e = min(max(__float_as_uint(largest) >> 23, 27u), 254u);
+  return {__uint_as_float((268u - e) << 23), __uint_as_float((e - 14u) << 23)};
+}
+__device__ inline float max_of(float a, float b) { return fmaxf(a, fabsf(b)); }
+template <int N>
+__device__ inline float largest_of(const float (&v)[N], float so_far = 0.f) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) so_far = max_of(so_far, v[j]);
+  return so_far;
+}
+// Largest of a lane and the one 32, or 16, lanes away.
+__device__ inline float max_over_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_over_16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float max_of_wave(float x) {
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return max_over_32(max_over_16(x));
+}
+
+struct Split {
+  u32x4 p[2];
+};
+template <bool WIDE>
+__device__ inline Split split8(const float (&v)[8], float scale) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
   Split s;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a = v[2 * i], b = v[2 * i + 1];
-#pragma unroll
-    for (int q = 0; q < 3; ++q) {
-      const uint32_t ab = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
-      s.p[q][i] = ab;
-      a -= __uint_as_float(ab << 16);
-      b -= __uint_as_float(ab & 0xffff0000u);
-    }
+    float a = v[2 * i] * scale, b = v[2 * i + 1] * scale;
+    const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
+    a -= (float)h[0];
+    b -= (float)h[1];
+    if (WIDE) a *= kWide, b *= kWide;
+    s.p[0][i] = __builtin_bit_cast(uint32_t, h);
+    s.p[1][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
   }
   return s;
 }
 
-__device__ inline Split split8(float (&v)[8], float sign) {
+// ---- products -----------------------------------------------------------------------------------
+__device__ inline f32x16 zeros() {
+  f32x16 z;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= sign;
-  return split8(v);
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
 }
-
 __device__ inline f32x16 mfma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-// c + a b, the small products first.
+// c + a b, both narrow, the small products first
 __device__ inline f32x16 product(const Split &a, const Split &b, f32x16 c) {
-  c = mfma(a.p[2], b.p[0], c);
-  c = mfma(a.p[0], b.p[2], c);
-  c = mfma(a.p[1], b.p[1], c);
   c = mfma(a.p[1], b.p[0], c);
   c = mfma(a.p[0], b.p[1], c);
   return mfma(a.p[0], b.p[0], c);
 }
+struct Sums {  // of wide products: main + cross / kWide
+  f32x16 main, cross;
+};
+__device__ inline Sums no_sums() { return {zeros(), zeros()}; }
+__device__ inline void add_product(Sums &c, const Split &a, const Split &b) {
+  c.cross = mfma(a.p[1], b.p[0], c.cross);
+  c.main = mfma(a.p[0], b.p[0], c.main);
+  c.cross = mfma(a.p[0], b.p[1], c.cross);
+}
 __device__ inline Split fragment(const u32x4 *at, int64_t index) {
   at += index * kFragment + (threadIdx.x & (kWave - 1));
-  return Split{{at[0], at[kWave], at[2 * kWave]}};
+  return Split{{at[0], at[kWave]}};
+}
+// The sums times what was divided out, and a vector with one value a row of the result.
+__device__ inline f32x16 value_of(const Sums &c, float inv, const float *per_row, int g) {
+  f32x16 z;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float4 t = *reinterpret_cast<const float4 *>(per_row + 8 * q + 4 * g);
+    const float b[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[4 * q + e] = fmaf(c.main[4 * q + e], inv, fmaf(c.cross[4 * q + e], inv * (1.f / kWide), b[e]));
+  }
+  return z;
+}
+__device__ inline f32x16 value_of(const Sums &c, float inv) {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = fmaf(c.main[r], inv, c.cross[r] * (inv * (1.f / kWide)));
+  return z;
+}
+__device__ inline void add(f32x16 &c, float factor, const f32x16 &x) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) c[r] = fmaf(factor, x[r], c[r]);
+}
+__device__ inline float largest_of(const f32x16 &x, float so_far = 0.f) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) so_far = max_of(so_far, x[r]);
+  return so_far;
+}
+template <bool WIDE>
+__device__ inline Split half(const f32x16 &r, int s, float scale) {  // the registers 8 s .. 8 s + 7 as an operand
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = r[8 * s + j];
+  return split8<WIDE>(v, scale);
 }
 
 // ---- the activations ----------------------------------------------------------------------------
-struct Sigmoid {
-  float s, rest;  // sigmoid and 1 - sigmoid, each to its own last bits
-};
-__device__ inline Sigmoid sigmoid2(float x) {
-  const float e = __expf(-fabsf(x)), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-  return x >= 0.f ? Sigmoid{big, small} : Sigmoid{small, big};
-}
-// The normal distribution's Phi(x), and its density times sqrt(2 pi).  The tail Q(t) = 1 - Phi(t), t >= 0, is exp(-t^2 / 2) times a function
-// that falls like 1 / t: a polynomial in k = 1 / (1 + 0.3 t) without a constant term, fitted for the least relative error (1.5e-7 over t <= 14,
-// 4.3e-7 with the arithmetic's own), so that both tails keep their last bits, where 1 + erf loses the lower one.
+// The normal distribution's tail Q(|x|) = 1 - Phi(|x|), and its density times sqrt(2 pi), exp(-x^2 / 2).  Q is that times a function that falls like
+// 1 / |x|: a polynomial in k = 1 / (1 + 0.275 |x|) without a constant term, fitted for the least error of |x| Q (1.1e-8, 6.9e-8 with the
+// arithmetic's own; of Q itself 4e-5 of it at most up to |x| = 4).  x Phi(x) = max(x, 0) - |x| Q(|x|) for either sign.
 struct Normal {
-  float cdf, density;
+  float tail, density;
 };
 __device__ inline Normal normal_of(float x) {
-  const float t = fabsf(x), k = __builtin_amdgcn_rcpf(fmaf(0.3f, t, 1.f)), e = __expf(-0.5f * x * x);
-  float q = 0.03567368909716606f;
-  q = fmaf(q, k, -0.15719902515411377f);
-  q = fmaf(q, k, 0.2063472718000412f);
-  q = fmaf(q, k, -0.05367852374911308f);
-  q = fmaf(q, k, 0.12855921685695648f);
-  q = fmaf(q, k, 0.09991414099931717f);
-  q = fmaf(q, k, 0.12075386196374893f);
-  q = fmaf(q, k, 0.11962930113077164f);
-  q *= k * e;
-  return {x < 0.f ? q : 1.f - q, e};
+  const float k = __builtin_amdgcn_rcpf(fmaf(0.275f, fabsf(x), 1.f)), e = __builtin_amdgcn_exp2f(x * x * -0.72134752f);
+  float q = -0.11416427046060562f;
+  q = fmaf(q, k, 0.44915953278541565f);
+  q = fmaf(q, k, -0.3263809084892273f);
+  q = fmaf(q, k, 0.3302135169506073f);
+  q = fmaf(q, k, 0.04359893128275871f);
+  q = fmaf(q, k, 0.11757319420576096f);
+  return {q * (k * e), e};
 }
+__device__ inline float relu_of(float x) { return x < 0.f ? 0.f : x; }  // (NaN stays)
 
 template <int ACT>
 __device__ inline float activate(float x) {
-  if (ACT == PIPAD_ACT_RELU) return x < 0.f ? 0.f : x;  // (NaN stays)
-  if (ACT == PIPAD_ACT_GELU) return x * normal_of(x).cdf;
+  if (ACT == PIPAD_ACT_RELU) return relu_of(x);
+  if (ACT == PIPAD_ACT_GELU) return fmaf(-fabsf(x), normal_of(x).tail, relu_of(x));
   const float s = __builtin_amdgcn_rcpf(1.f + __expf(-x));
   return ACT == PIPAD_ACT_SIGMOID ? s : x * s;
 }
 // act(x) and its slope
 template <int ACT>
 __device__ inline float2 activate_slope(float x) {
-  if (ACT == PIPAD_ACT_RELU) return make_float2(x < 0.f ? 0.f : x, x > 0.f ? 1.f : 0.f);
+  if (ACT == PIPAD_ACT_RELU) return make_float2(relu_of(x), x > 0.f ? 1.f : 0.f);
   if (ACT == PIPAD_ACT_GELU) {
     const Normal p = normal_of(x);
-    return make_float2(x * p.cdf, fmaf(x * 0.39894228f, p.density, p.cdf));
+    return make_float2(fmaf(-fabsf(x), p.tail, relu_of(x)), fmaf(x * 0.39894228f, p.density, x < 0.f ? p.tail : 1.f - p.tail));
   }
-  const Sigmoid s = sigmoid2(x);
-  if (ACT == PIPAD_ACT_SIGMOID) return make_float2(s.s, s.s * s.rest);
-  return make_float2(x * s.s, s.s * fmaf(x, s.rest, 1.f));
+  const float s = __builtin_amdgcn_rcpf(1.f + __expf(-x)), rest = 1.f - s;
+  if (ACT == PIPAD_ACT_SIGMOID) return make_float2(s, s * rest);
+  const float a = x * s;
+  return make_float2(a, fmaf(a, rest, s));
 }
 
 // ---- arguments ----------------------------------------------------------------------------------
@@ -141,9 +221,9 @@ struct FfArgs {
   int32_t n, k, F, hidden, Fo;
   int32_t ht, fq, oq, ft, ot;  // 32-column tiles of the hidden columns, 16- and 32-column tiles of X's and Y's
   bool vec_x, vec_dy, vec_o;
-  // Weights as fragments.  gu: [ht], each [fq][Wg, Wu], m = hidden column, depth = X's columns, and behind them the biases of the tile's
-  // hidden columns (32 floats of bg, 32 of bu, 256 bytes unused), 0 where there are none.  down: [ht][ot][2], m = Y's column, depth of a
-  // result = hidden.  up: [ht][oq], m = hidden, depth = Y's columns (Wd).  back: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
+  // Weights as fragments.  gu, wide: [ht], each [fq][Wg, Wu], m = hidden column, depth = X's columns, and a TileVectors behind them.
+  // up, wide: [ht][oq], m = hidden, depth = Y's columns (Wd).  down, narrow: [ht][ot][2], m = Y's column, depth of a result = hidden.
+  // back, narrow: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
   const u32x4 *gu, *down, *up, *back;
   const float *bd;  // padded with zeros to whole tiles
   const float *Wg, *Wu, *Wd, *bg, *bu;  // as they came
@@ -152,6 +232,7 @@ struct FfArgs {
   float *partial;
   int64_t part_floats, tiles_per_part;
 };
+__device__ inline const TileVectors &vectors_of(const u32x4 *gu, int fq) { return *reinterpret_cast<const TileVectors *>(gu + fq * 2 * kFragment); }
 
 struct RowAt {
   int32_t t, i;
@@ -177,15 +258,18 @@ __device__ inline void load8(float (&v)[8], const float *p, int c, int F, bool v
     }
   }
 }
-__device__ inline f32x16 zeros() {
-  f32x16 z;
+// A row of up to 16 N columns, whose other half lane m + 32 has, as wide pieces; returns 1 over its scale.
+template <int N>
+__device__ inline float load_row(Split (&x)[N], const float *row, int g, int F, bool vec) {
+  float v[N][8], largest = 0.f;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) z[r] = 0.f;
-  return z;
-}
-__device__ inline void add(f32x16 &c, float sign, const f32x16 &x) {
+  for (int q = 0; q < N; ++q) load8(v[q], row, q * kDepth + 8 * g, F, vec);
 #pragma unroll
-  for (int r = 0; r < 16; ++r) c[r] = fmaf(sign, x[r], c[r]);
+  for (int q = 0; q < N; ++q) largest = largest_of(v[q], largest);
+  const Scale s = scale_for(max_over_32(largest));
+#pragma unroll
+  for (int q = 0; q < N; ++q) x[q] = split8<true>(v[q], s.to);
+  return s.inv;
 }
 // A column vector, one value a row of a result.
 __device__ inline f32x16 per_row(const float *p, int g) {
@@ -196,12 +280,6 @@ __device__ inline f32x16 per_row(const float *p, int g) {
     z[4 * q] = t.x, z[4 * q + 1] = t.y, z[4 * q + 2] = t.z, z[4 * q + 3] = t.w;
   }
   return z;
-}
-__device__ inline Split half(const f32x16 &r, int s) {  // the registers 8 s .. 8 s + 7 as an operand
-  float v[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = r[8 * s + j];
-  return split8(v);
 }
 // A result's rows are columns c0 .. of a matrix, its column m a row of it.
 __device__ inline void store_tile(const f32x16 &r, float *row, int c0, int F, bool vec, int g) {

@@ -12,67 +12,102 @@ struct PackArgs {
   const float *Wg, *Wu, *Wd, *bg, *bu, *bd;
   int64_t ldwg, ldwu, ldwd;
   int32_t F, hidden, Fo, ht, fq, oq, ft, ot;
-  int64_t n_gu, n_down, n_up, n_back;  // fragments of each kind (0: not wanted)
-  u32x4 *gu, *down, *up, *back;
+  u32x4 *gu, *down, *up, *back;  // (all but gu: null where they are not wanted)
   float *pbd;
 };
-__global__ void __launch_bounds__(kBlock) k_ff_pack(PackArgs a) {
-  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
-  int64_t at = ((int64_t)blockIdx.x * kBlock + threadIdx.x) / kWave;
-  if (at == 0)  // the last bias, by the first wave
-    for (int c = lane; c < a.ot * kTile; c += kWave) a.pbd[c] = a.bd && c < a.Fo ? a.bd[c] : 0.f;
-  float v[8];
-  u32x4 *to;
-  if (at < a.n_gu) {
-    const int w = (int)(at % 2), q = (int)(at / 2 % a.fq), h = (int)(at / 2 / a.fq);
-    const float *W = w ? a.Wu : a.Wg;
-    const int64_t ld = w ? a.ldwu : a.ldwg;
-    const int hid = h * kTile + m;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int f = q * kDepth + 8 * g + j;
-      v[j] = f < a.F && hid < a.hidden ? W[f * ld + hid] : 0.f;
-    }
-    to = a.gu + (int64_t)h * gu_words(a.fq) + (at - (int64_t)h * a.fq * 2) * kFragment;
-    if (at == (int64_t)h * a.fq * 2) {  // the tile's biases, by the wave of its first fragment
-      const float *const b = g ? a.bu : a.bg;
-      reinterpret_cast<float *>(a.gu + (int64_t)h * gu_words(a.fq) + a.fq * 2 * kFragment)[lane] = b && hid < a.hidden ? b[hid] : 0.f;
-    }
-  } else if ((at -= a.n_gu) < a.n_down) {
-    const int s = (int)(at % 2), o = (int)(at / 2 % a.ot), h = (int)(at / 2 / a.ot), fo = o * kTile + m;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int hid = h * kTile + result_depth(s, g, j);
-      v[j] = hid < a.hidden && fo < a.Fo ? a.Wd[hid * a.ldwd + fo] : 0.f;
-    }
-    to = a.down + at * kFragment;
-  } else if ((at -= a.n_down) < a.n_up) {
-    const int q = (int)(at % a.oq), h = (int)(at / a.oq), hid = h * kTile + m;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int fo = q * kDepth + 8 * g + j;
-      v[j] = hid < a.hidden && fo < a.Fo ? a.Wd[hid * a.ldwd + fo] : 0.f;
-    }
-    to = a.up + at * kFragment;
-  } else if ((at -= a.n_up) < a.n_back) {
-    const int w = (int)(at % 2), s = (int)(at / 2 % 2), t = (int)(at / 4 % a.ft), h = (int)(at / 4 / a.ft), f = t * kTile + m;
-    const float *W = w ? a.Wu : a.Wg;
-    const int64_t ld = w ? a.ldwu : a.ldwg;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int hid = h * kTile + result_depth(s, g, j);
-      v[j] = hid < a.hidden && f < a.F ? W[f * ld + hid] : 0.f;
-    }
-    to = a.back + at * kFragment;
-  } else {
-    return;
+// A workgroup a hidden tile: the largest of its weights, then a wave a fragment.
+constexpr int kPackWaves = 16;
+__global__ void __launch_bounds__(kPackWaves *kWave) k_ff_pack(PackArgs a) {
+  __shared__ float found[2][kPackWaves];
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int h = blockIdx.x, h0 = h * kTile;
+  {
+    float gu = 0.f, down = 0.f;
+    if (h0 + m < a.hidden)
+      for (int f = 2 * wave + g; f < a.F; f += 2 * kPackWaves) gu = max_of(max_of(gu, a.Wg[f * a.ldwg + h0 + m]), a.Wu[f * a.ldwu + h0 + m]);
+    for (int r = h0 + wave; r < a.hidden && r < h0 + kTile; r += kPackWaves)
+      for (int c = lane; c < a.Fo; c += kWave) down = max_of(down, a.Wd[r * a.ldwd + c]);
+    gu = max_of_wave(gu), down = max_of_wave(down);
+    if (lane == 0) found[0][wave] = gu, found[1][wave] = down;
   }
-  const Split s = split8(v);
+  __syncthreads();
+  float gu = 0.f, down = 0.f;
 #pragma unroll
-  for (int q = 0; q < 3; ++q) to[q * kWave + lane] = s.p[q];
+  for (int w = 0; w < kPackWaves; ++w) gu = fmaxf(gu, found[0][w]), down = fmaxf(down, found[1][w]);
+  const Scale scale_gu = scale_for(gu), scale_down = scale_for(down);
+  u32x4 *const tile = a.gu + (int64_t)h * gu_words(a.fq);
+  if (threadIdx.x < kWave) {
+    TileVectors &t = *reinterpret_cast<TileVectors *>(tile + a.fq * 2 * kFragment);
+    const float *const b = g ? a.bu : a.bg;
+    (g ? t.bu : t.bg)[m] = b && h0 + m < a.hidden ? b[h0 + m] : 0.f;
+    if (lane == 0) t.inv_gu = t.inv_back = scale_gu.inv, t.inv_up = t.inv_down = scale_down.inv;
+  }
+  if (h == 0)
+    for (int c = threadIdx.x; c < a.ot * kTile; c += kPackWaves * kWave) a.pbd[c] = a.bd && c < a.Fo ? a.bd[c] : 0.f;
+
+  const int n_gu = 2 * a.fq, n_down = a.down ? 2 * a.ot : 0, n_up = a.up ? a.oq : 0, n_back = a.back ? 4 * a.ft : 0;
+  for (int at = wave; at < n_gu + n_down + n_up + n_back; at += kPackWaves) {
+    float v[8];
+    Split s;
+    u32x4 *to;
+    int q = at;
+    if (q < n_gu) {  // [fq][Wg, Wu]
+      const float *W = q % 2 ? a.Wu : a.Wg;
+      const int64_t ld = q % 2 ? a.ldwu : a.ldwg;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int f = q / 2 * kDepth + 8 * g + j;
+        v[j] = f < a.F && h0 + m < a.hidden ? W[f * ld + h0 + m] : 0.f;
+      }
+      s = split8<true>(v, scale_gu.to);
+      to = tile + q * kFragment;
+    } else if ((q -= n_gu) < n_down) {  // [ot][2]
+      const int fo = q / 2 * kTile + m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int hid = h0 + result_depth(q % 2, g, j);
+        v[j] = hid < a.hidden && fo < a.Fo ? a.Wd[hid * a.ldwd + fo] : 0.f;
+      }
+      s = split8<false>(v, scale_down.to);
+      to = a.down + ((int64_t)h * n_down + q) * kFragment;
+    } else if ((q -= n_down) < n_up) {  // [oq]
+      if (h0 + m < a.hidden) {
+        load8(v, a.Wd + (h0 + m) * a.ldwd, q * kDepth + 8 * g, a.Fo, false);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.f;
+      }
+      s = split8<true>(v, scale_down.to);
+      to = a.up + ((int64_t)h * n_up + q) * kFragment;
+    } else {  // [ft][2][Wg, Wu]
+      q -= n_up;
+      const int f = q / 4 * kTile + m;
+      const float *W = q % 2 ? a.Wu : a.Wg;
+      const int64_t ld = q % 2 ? a.ldwu : a.ldwg;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int hid = h0 + result_depth(q / 2 % 2, g, j);
+        v[j] = hid < a.hidden && f < a.F ? W[f * ld + hid] : 0.f;
+      }
+      s = split8<false>(v, scale_gu.to);
+      to = a.back + ((int64_t)h * n_back + q) * kFragment;
+    }
+#pragma unroll
+    for (int p = 0; p < 2; ++p) to[p * kWave + lane] = s.p[p];
+  }
 }
 
 // ---- forward ------------------------------------------------------------------------------------
+// Scale of a row of any width, of which lane m + 32 has the other half of every 16 columns.
+__device__ inline Scale scale_of_row(const float *row, int F, int g, bool vec) {
+  float largest = 0.f, v[8];
+  for (int c = 8 * g; c < F; c += kDepth) {
+    load8(v, row, c, F, vec);
+    largest = largest_of(v, largest);
+  }
+  return scale_for(max_over_32(largest));
+}
+
 // A wave: 32 node rows, OT tiles of Y's columns from tile blockIdx.y * OT on.  Results lie transposed (a node row is a lane's column).
 template <int ACT, int OT>
 __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
@@ -81,30 +116,35 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
   if (base >= a.rows) return;
   const RowAt at = row_at(a, base, m);
   const float *const x = a.X[at.t] + at.i * a.ldx;
+  const Scale scale_x = scale_of_row(x, a.F, g, a.vec_x);
   const int o0 = blockIdx.y * OT;
   f32x16 y[OT];
 #pragma unroll
   for (int o = 0; o < OT; ++o) y[o] = o0 + o < a.ot ? per_row(a.bd + (o0 + o) * kTile, g) : zeros();
   for (int h = 0; h < a.ht; ++h) {
     const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
-    const float *const bias = reinterpret_cast<const float *>(gu + a.fq * 2 * kFragment);
-    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g);
+    const TileVectors &vectors = vectors_of(gu, a.fq);
+    Sums sg = no_sums(), su = no_sums();
     for (int q = 0; q < a.fq; ++q) {
       float v[8];
       load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
-      const Split b = split8(v);
-      G = product(fragment(gu, 2 * q), b, G);
-      U = product(fragment(gu, 2 * q + 1), b, U);
+      const Split b = split8<true>(v, scale_x.to);
+      add_product(sg, fragment(gu, 2 * q), b);
+      add_product(su, fragment(gu, 2 * q + 1), b);
     }
+    const float inv = scale_x.inv * vectors.inv_gu;
+    f32x16 G = value_of(sg, inv, vectors.bg, g);
+    const f32x16 U = value_of(su, inv, vectors.bu, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
+    const Scale scale = scale_for(max_over_32(largest_of(G)));
+    const Split b[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)};
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const Split b = half(G, s);
-#pragma unroll
-      for (int o = 0; o < OT; ++o)
-        if (o0 + o < a.ot) y[o] = product(fragment(a.down, ((int64_t)h * a.ot + o0 + o) * 2 + s), b, y[o]);
-    }
+    for (int o = 0; o < OT; ++o)
+      if (o0 + o < a.ot) {
+        const int64_t w = ((int64_t)h * a.ot + o0 + o) * 2;
+        add(y[o], scale.inv * vectors.inv_down, product(fragment(a.down, w + 1), b[1], product(fragment(a.down, w), b[0], zeros())));
+      }
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
@@ -120,42 +160,48 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
   if (base >= a.rows) return;
   const RowAt at = row_at(a, base, m);
   const float *const x = a.X[at.t] + at.i * a.ldx, *const dy = a.dY[at.t] + at.i * a.lddy;
+  const Scale scale_x = scale_of_row(x, a.F, g, a.vec_x), scale_dy = scale_of_row(dy, a.Fo, g, a.vec_dy);
   const int f0 = blockIdx.y * FT;
   f32x16 dx[FT];
 #pragma unroll
   for (int f = 0; f < FT; ++f) dx[f] = zeros();
   for (int h = 0; h < a.ht; ++h) {
     const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
-    const float *const bias = reinterpret_cast<const float *>(gu + a.fq * 2 * kFragment);
-    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g), dH = zeros();
+    const TileVectors &vectors = vectors_of(gu, a.fq);
+    Sums sg = no_sums(), su = no_sums(), sd = no_sums();
     float v[8];
     for (int q = 0; q < a.fq; ++q) {
       load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
-      const Split b = split8(v);
-      G = product(fragment(gu, 2 * q), b, G);
-      U = product(fragment(gu, 2 * q + 1), b, U);
+      const Split b = split8<true>(v, scale_x.to);
+      add_product(sg, fragment(gu, 2 * q), b);
+      add_product(su, fragment(gu, 2 * q + 1), b);
     }
     for (int q = 0; q < a.oq; ++q) {
       load8(v, dy, q * kDepth + 8 * g, a.Fo, a.vec_dy);
-      dH = product(fragment(a.up, (int64_t)h * a.oq + q), split8(v), dH);
+      add_product(sd, fragment(a.up, (int64_t)h * a.oq + q), split8<true>(v, scale_dy.to));
     }
+    const float inv = scale_x.inv * vectors.inv_gu;
+    f32x16 G = value_of(sg, inv, vectors.bg, g), U = value_of(su, inv, vectors.bu, g);
+    const f32x16 dH = value_of(sd, scale_dy.inv * vectors.inv_up);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float2 c = activate_slope<ACT>(G[r]);
       G[r] = dH[r] * U[r] * c.y;
       U[r] = dH[r] * c.x;
     }
+    const Scale scale = scale_for(max_over_32(largest_of(U, largest_of(G))));
+    const Split dg[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)}, du[2] = {half<false>(U, 0, scale.to), half<false>(U, 1, scale.to)};
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const Split dg = half(G, s), du = half(U, s);
+    for (int f = 0; f < FT; ++f)
+      if (f0 + f < a.ft) {
+        f32x16 sum = zeros();
 #pragma unroll
-      for (int f = 0; f < FT; ++f)
-        if (f0 + f < a.ft) {
+        for (int s = 0; s < 2; ++s) {
           const int64_t w = (((int64_t)h * a.ft + f0 + f) * 2 + s) * 2;
-          dx[f] = product(fragment(a.back, w), dg, dx[f]);
-          dx[f] = product(fragment(a.back, w + 1), du, dx[f]);
+          sum = product(fragment(a.back, w + 1), du[s], product(fragment(a.back, w), dg[s], sum));
         }
-    }
+        add(dx[f], scale.inv * vectors.inv_back, sum);
+      }
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
@@ -165,20 +211,21 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
 
 // ---- the gradients of the weights ---------------------------------------------------------------
 // A wave: one tile of hidden columns, the rows of one part, T tiles of X's and of Y's columns from tile blockIdx.z * T on.  Results
-// lie as they are (a hidden column is a lane's column), so dG, dU and H are operands of products whose depth is the node rows.
+// lie as they are (a hidden column is a lane's column), so dG, dU and H are operands of products whose depth is the node rows; X and dY keep their
+// rows' scales there, by whose inverses dG, dU and H are multiplied before they get a scale of their own, a hidden column each.
 template <int ACT, int T>
 __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
   const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
   const int h = blockIdx.x * kWavesPerBlock + threadIdx.x / kWave;
   if (h >= a.ht) return;
   const int t0 = blockIdx.z * T;
-  f32x16 dwg[T], dwu[T], dwd[T];
+  f32x16 dwg[T], dwu[T], dwd[T];  // dwd transposed: its rows are Y's columns
 #pragma unroll
   for (int t = 0; t < T; ++t) dwg[t] = dwu[t] = dwd[t] = zeros();
   float dbg = 0.f, dbu = 0.f, dbd[T] = {};
   const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
-  const float *const bias = reinterpret_cast<const float *>(gu + a.fq * 2 * kFragment);
-  const float bg = bias[m], bu = bias[kTile + m];
+  const TileVectors &vectors = vectors_of(gu, a.fq);
+  const float bg = vectors.bg[m], bu = vectors.bu[m];
   const int64_t first = blockIdx.y * a.tiles_per_part * kTile;
   const int64_t end = first + a.tiles_per_part * kTile < a.rows ? first + a.tiles_per_part * kTile : a.rows;
   for (int64_t base = first; base < end; base += kTile) {
@@ -186,71 +233,88 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
     const RowAt at = row_at(a, base, m);
     const float *const x = a.X[at.t] + at.i * a.ldx, *const dy = a.dY[at.t] + at.i * a.lddy;
     const float sign = base / kTile % 2 ? -1.f : 1.f;
-    f32x16 G, U, dH = zeros();
-#pragma unroll
-    for (int r = 0; r < 16; ++r) G[r] = sign * bg, U[r] = sign * bu;
+    const Scale scale_x = scale_of_row(x, there ? a.F : 0, g, a.vec_x), scale_dy = scale_of_row(dy, there ? a.Fo : 0, g, a.vec_dy);
+    Sums sg = no_sums(), su = no_sums(), sd = no_sums();
     float v[8];
     for (int q = 0; q < a.fq; ++q) {
       load8(v, x, q * kDepth + 8 * g, there ? a.F : 0, a.vec_x);
-      const Split b = split8(v, sign);
-      G = product(b, fragment(gu, 2 * q), G);
-      U = product(b, fragment(gu, 2 * q + 1), U);
+      const Split b = split8<true>(v, sign * scale_x.to);
+      add_product(sg, b, fragment(gu, 2 * q));
+      add_product(su, b, fragment(gu, 2 * q + 1));
     }
     for (int q = 0; q < a.oq; ++q) {
       load8(v, dy, q * kDepth + 8 * g, there ? a.Fo : 0, a.vec_dy);
-      dH = product(split8(v, sign), fragment(a.up, (int64_t)h * a.oq + q), dH);
+      add_product(sd, split8<true>(v, sign * scale_dy.to), fragment(a.up, (int64_t)h * a.oq + q));
     }
+    float vg[16], vu[16], vh[16], to_x[16], to_dy[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float2 c = activate_slope<ACT>(sign * G[r]);
-      const float u = sign * U[r], d = sign * dH[r];
-      G[r] = d * u * c.y;
-      U[r] = d * c.x;
-      dH[r] = c.x * u;
-      dbg += G[r];
-      dbu += U[r];
+      const int d = result_depth(r / 8, g, r % 8);
+      const float inv_x = __shfl(scale_x.inv, d), inv_dy = __shfl(scale_dy.inv, d);
+      to_x[r] = __shfl(scale_x.to, d), to_dy[r] = __shfl(scale_dy.to, d);
+      const float cx = sign * vectors.inv_gu * inv_x, cd = sign * vectors.inv_up * inv_dy;
+      const float2 c = activate_slope<ACT>(fmaf(sg.main[r], cx, fmaf(sg.cross[r], cx * (1.f / kWide), bg)));
+      const float u = fmaf(su.main[r], cx, fmaf(su.cross[r], cx * (1.f / kWide), bu)), e = fmaf(sd.main[r], cd, sd.cross[r] * (cd * (1.f / kWide)));
+      vg[r] = e * u * c.y;
+      vu[r] = e * c.x;
+      dbg += vg[r];
+      dbu += vu[r];
+      vg[r] *= inv_x;
+      vu[r] *= inv_x;
+      vh[r] = c.x * u * inv_dy;
     }
-    Split dg[2], du[2], hh[2];
-    RowAt rows[2][8];
-    bool in[2][8];
+    const auto pieces = [&](const float (&from)[16], Split (&to)[2]) {
+      const Scale scale = scale_for(max_over_32(largest_of(from)));
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      dg[s] = half(G, s), du[s] = half(U, s), hh[s] = half(dH, s);
+      for (int s = 0; s < 2; ++s) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int d = result_depth(s, g, j);
-        rows[s][j] = row_at(a, base, d);
-        in[s][j] = base + d < end;
+        for (int j = 0; j < 8; ++j) v[j] = from[8 * s + j];
+        to[s] = split8<true>(v, scale.to);
       }
-    }
+      return sign * scale.inv;
+    };
+    Split dg[2], du[2], hh[2];
+    const float cg = pieces(vg, dg), cu = pieces(vu, du), ch = pieces(vh, hh);
+    const auto add_sums = [&](f32x16 &to, float factor, const Sums &c) {
+      add(to, factor * (1.f / kWide), c.cross);
+      add(to, factor, c.main);
+    };
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const int c = (t0 + t) * kTile + m;
+      const auto transposed = [&](const float *const *X, int64_t ld, int F, const float (&to)[16], int s) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int d = result_depth(s, g, j);
+          const RowAt r = row_at(a, base, d);
+          v[j] = base + d < end && c < F ? X[r.t][r.i * ld + c] : 0.f;
+        }
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = v[j] * to[8 * s + j];
+        return split8<true>(w, sign);
+      };
       if (t0 + t < a.ft) {
-        f32x16 g_sum = zeros(), u_sum = zeros();
+        Sums g_sum = no_sums(), u_sum = no_sums();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[j] = in[s][j] && c < a.F ? a.X[rows[s][j].t][rows[s][j].i * a.ldx + c] : 0.f;
-          const Split xs = split8(v, sign);
-          g_sum = product(xs, dg[s], g_sum);
-          u_sum = product(xs, du[s], u_sum);
+          const Split xs = transposed(a.X, a.ldx, a.F, to_x, s);
+          add_product(g_sum, xs, dg[s]);
+          add_product(u_sum, xs, du[s]);
         }
-        add(dwg[t], sign, g_sum);
-        add(dwu[t], sign, u_sum);
+        add_sums(dwg[t], cg, g_sum);
+        add_sums(dwu[t], cu, u_sum);
       }
       if (t0 + t < a.ot) {
-        f32x16 d_sum = zeros();
+        Sums d_sum = no_sums();
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
+          const Split ds = transposed(a.dY, a.lddy, a.Fo, to_dy, s);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            v[j] = in[s][j] && c < a.Fo ? a.dY[rows[s][j].t][rows[s][j].i * a.lddy + c] : 0.f;
-            dbd[t] += v[j];
-          }
-          d_sum = product(hh[s], split8(v, sign), d_sum);
+          for (int j = 0; j < 8; ++j) dbd[t] += v[j];
+          add_product(d_sum, ds, hh[s]);
         }
-        add(dwd[t], sign, d_sum);
+        add_sums(dwd[t], ch, d_sum);
       }
     }
   }
@@ -260,13 +324,12 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
   for (int t = 0; t < T; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = result_depth(r / 8, g, r % 8), f = (t0 + t) * kTile + row;
-      if (f < a.F && hid < a.hidden) {
-        to[(int64_t)f * a.hidden + hid] = dwg[t][r];
-        to[((int64_t)a.F + f) * a.hidden + hid] = dwu[t][r];
+      const int c = (t0 + t) * kTile + result_depth(r / 8, g, r % 8);
+      if (c < a.F && hid < a.hidden) {
+        to[(int64_t)c * a.hidden + hid] = dwg[t][r];
+        to[((int64_t)a.F + c) * a.hidden + hid] = dwu[t][r];
       }
-      const int fo = (t0 + t) * kTile + m;
-      if (h * kTile + row < a.hidden && fo < a.Fo) to_d[(int64_t)(h * kTile + row) * a.Fo + fo] = dwd[t][r];
+      if (c < a.Fo && hid < a.hidden) to_d[(int64_t)hid * a.Fo + c] = dwd[t][r];
     }
   float *const to_b = to_d + (int64_t)a.hidden * a.Fo;
   dbg += __shfl_xor(dbg, 32);
@@ -395,28 +458,23 @@ FfArgs arguments(const pipad_gated_ff_t &c, const Plan &p, int32_t n, int32_t k,
 }
 
 int pack(const pipad_gated_ff_t &c, const Plan &p, char *ws, hipStream_t st) {
-  PackArgs a{c.Wg,   c.Wu,   c.Wd,     c.bg,   c.bu,
-             c.bd,   c.ldwg, c.ldwu,   c.ldwd, c.F,
-             c.hidden, c.Fo, p.ht,     p.fq,   p.oq,
-             p.ft,   p.ot,   p.n_gu,   p.n_down, p.n_up,
-             p.n_back, reinterpret_cast<u32x4 *>(ws + p.gu), reinterpret_cast<u32x4 *>(ws + p.down), reinterpret_cast<u32x4 *>(ws + p.up),
-             reinterpret_cast<u32x4 *>(ws + p.back), reinterpret_cast<float *>(ws + p.bd)};
-  const int64_t waves = p.n_gu + p.n_down + p.n_up + p.n_back;
-  hipLaunchKernelGGL(k_ff_pack, dim3((unsigned)tiles(waves, kWavesPerBlock)), dim3(kBlock), 0, st, a);
+  const auto at = [&](size_t offset, int64_t count) { return count ? reinterpret_cast<u32x4 *>(ws + offset) : nullptr; };
+  const PackArgs a{c.Wg,   c.Wu,   c.Wd, c.bg, c.bu, c.bd, c.ldwg, c.ldwu, c.ldwd, c.F, c.hidden, c.Fo,
+                   p.ht,   p.fq,   p.oq, p.ft, p.ot, at(p.gu, p.n_gu), at(p.down, p.n_down), at(p.up, p.n_up), at(p.back, p.n_back),
+                   reinterpret_cast<float *>(ws + p.bd)};
+  hipLaunchKernelGGL(k_ff_pack, dim3((unsigned)p.ht), dim3(kPackWaves * kWave), 0, st, a);
   PIPAD_HIP(hipGetLastError());
   return PIPAD_OK;
 }
 
-// A kernel by activation and by the tiles of columns that a wave keeps: 1, 2 or 4.
-#define PIPAD_FF_KERNELS(name)                                                                                                        \
-  using name##_fn = void (*)(FfArgs);                                                                                                 \
-  constexpr name##_fn name##_of[4][3] = {{name<0, 1>, name<0, 2>, name<0, 4>},                                                        \
-                                         {name<1, 1>, name<1, 2>, name<1, 4>},                                                        \
-                                         {name<2, 1>, name<2, 2>, name<2, 4>},                                                        \
-                                         {name<3, 1>, name<3, 2>, name<3, 4>}};
-PIPAD_FF_KERNELS(k_ff_rows)
-PIPAD_FF_KERNELS(k_ff_rows_backward)
-PIPAD_FF_KERNELS(k_ff_weights_backward)
+// A kernel by activation and by the tiles of columns that a wave keeps: 1, 2 or 4 (the weights' gradients, three matrices of them: 1 or 2).
+using FfKernel = void (*)(FfArgs);
+#define PIPAD_FF_KERNELS(name, ...) \
+  constexpr FfKernel name##_of[4][3] = {{name<0, 1>, name<0, 2>, name<0, __VA_ARGS__>}, {name<1, 1>, name<1, 2>, name<1, __VA_ARGS__>}, \
+                                        {name<2, 1>, name<2, 2>, name<2, __VA_ARGS__>}, {name<3, 1>, name<3, 2>, name<3, __VA_ARGS__>}};
+PIPAD_FF_KERNELS(k_ff_rows, 4)
+PIPAD_FF_KERNELS(k_ff_rows_backward, 4)
+PIPAD_FF_KERNELS(k_ff_weights_backward, 2)
 #undef PIPAD_FF_KERNELS
 
 int width(int t) { return t <= 1 ? 0 : t <= 2 ? 1 : 2; }  // which of 1, 2, 4 tiles
@@ -468,7 +526,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
       hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(c.hidden, 16 * f.waves), (unsigned)p.parts), dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());
     } else if (grads) {
-      const int most = std::max(p.ft, p.ot), w = width(most);
+      const int most = std::max(p.ft, p.ot), w = std::min(width(most), 1);
       hipLaunchKernelGGL(k_ff_weights_backward_of[c.activation][w],
                          dim3((unsigned)tiles(p.ht, kWavesPerBlock), (unsigned)p.parts, (unsigned)tiles(most, 1 << w)), dim3(kBlock), 0, st, a);
       PIPAD_HIP(hipGetLastError());

@@ -6,8 +6,8 @@ namespace ff {
 
 namespace {
 
-// The same where rows are 128 columns at most (see k_ff_kept): X's and dY's pieces stay in registers; the phases of a hidden tile are
-// [Wg, Wu, biases, Wd] and [Wg, Wu] laid out for the way back.
+// As the forward kernel: X's and dY's pieces stay in registers; the phases of a hidden tile are [Wg, Wu, vectors, Wd] and [Wg, Wu] laid out for
+// the way back.
 template <int ACT, int FQ, int OQ, int WAVES>
 __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_backward(FfArgs a) {
   constexpr int FT = FQ <= 2 ? 1 : FQ / 2;
@@ -19,56 +19,46 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_
   stage<WAVES, kUp>(a.up, in + kGu);
   const RowAt at = row_at(a, base < a.rows ? base : a.rows - 1, m);
   Split x[FQ], dy[OQ];
-  {
-    const float *const row = a.X[at.t] + at.i * a.ldx;
-    float v[FQ][8];
-#pragma unroll
-    for (int q = 0; q < FQ; ++q) load8(v[q], row, q * kDepth + 8 * g, a.F, a.vec_x);
-#pragma unroll
-    for (int q = 0; q < FQ; ++q) x[q] = split8(v[q]);
-  }
-  {
-    const float *const row = a.dY[at.t] + at.i * a.lddy;
-    float v[OQ][8];
-#pragma unroll
-    for (int q = 0; q < OQ; ++q) load8(v[q], row, q * kDepth + 8 * g, a.Fo, a.vec_dy);
-#pragma unroll
-    for (int q = 0; q < OQ; ++q) dy[q] = split8(v[q]);
-  }
+  const float inv_x = load_row(x, a.X[at.t] + at.i * a.ldx, g, a.F, a.vec_x);
+  const float inv_dy = load_row(dy, a.dY[at.t] + at.i * a.lddy, g, a.Fo, a.vec_dy);
   f32x16 dx[FT];
 #pragma unroll
   for (int f = 0; f < FT; ++f) dx[f] = zeros();
-  const float *const bias = reinterpret_cast<const float *>(in + FQ * 2 * kFragment);
   for (int h = 0; h < a.ht; ++h) {
     staged();
     stage<WAVES, kBack>(a.back + (int64_t)h * kBack, back);
-    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g), dH = zeros();
+    Sums sg = no_sums(), su = no_sums();
 #pragma unroll
     for (int q = 0; q < FQ; ++q) {
-      G = product(fragment(in, 2 * q), x[q], G);
-      U = product(fragment(in, 2 * q + 1), x[q], U);
+      add_product(sg, fragment(in, 2 * q), x[q]);
+      add_product(su, fragment(in, 2 * q + 1), x[q]);
     }
+    const TileVectors &v = vectors_of(in, FQ);
+    const float inv = inv_x * v.inv_gu, inv_back = v.inv_back;
+    f32x16 G = value_of(sg, inv, v.bg, g), U = value_of(su, inv, v.bu, g);
+    Sums sd = no_sums();
 #pragma unroll
-    for (int q = 0; q < OQ; ++q) dH = product(fragment(in + kGu, q), dy[q], dH);
+    for (int q = 0; q < OQ; ++q) add_product(sd, fragment(in + kGu, q), dy[q]);
+    const f32x16 dH = value_of(sd, inv_dy * v.inv_up);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float2 c = activate_slope<ACT>(G[r]);
       G[r] = dH[r] * U[r] * c.y;
       U[r] = dH[r] * c.x;
     }
+    const Scale scale = scale_for(max_over_32(largest_of(U, largest_of(G))));
+    const Split dg[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)}, du[2] = {half<false>(U, 0, scale.to), half<false>(U, 1, scale.to)};
     staged();
     if (h + 1 < a.ht) {
       stage<WAVES, kGu>(a.gu + (int64_t)(h + 1) * kGu, in);
       stage<WAVES, kUp>(a.up + (int64_t)(h + 1) * kUp, in + kGu);
     }
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const Split dg = half(G, s), du = half(U, s);
+    for (int f = 0; f < FT; ++f) {
+      f32x16 sum = zeros();
 #pragma unroll
-      for (int f = 0; f < FT; ++f) {
-        dx[f] = product(fragment(back, (f * 2 + s) * 2), dg, dx[f]);
-        dx[f] = product(fragment(back, (f * 2 + s) * 2 + 1), du, dx[f]);
-      }
+      for (int s = 0; s < 2; ++s) sum = product(fragment(back, (f * 2 + s) * 2 + 1), du[s], product(fragment(back, (f * 2 + s) * 2), dg[s], sum));
+      add(dx[f], scale.inv * inv_back, sum);
     }
   }
   if (base + m >= a.rows) return;

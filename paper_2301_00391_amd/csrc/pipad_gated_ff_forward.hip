@@ -6,9 +6,9 @@ namespace ff {
 
 namespace {
 
-// The same where a row's columns, and those of its result, are 128 at most: X's pieces stay in registers, and the waves of a workgroup, 32 node
-// rows each, share the weights through LDS.  A hidden tile's weights come in two phases, [Wg, Wu, biases] and [Wd], each into a buffer of its
-// own while the other is multiplied: loaded past the registers, one barrier a phase.  What is in flight is waited for before the barrier.
+// X's pieces stay in registers, and the waves of a workgroup, 32 node rows each, share the weights through LDS.  A hidden tile's weights come in
+// two phases, [Wg, Wu, vectors] and [Wd], each into a buffer of its own while the other is multiplied: loaded past the registers, one
+// barrier a phase.
 template <int ACT, int FQ, int OT, int WAVES>
 __global__ void __launch_bounds__(WAVES *kWave, 2) k_ff_kept(FfArgs a) {
   constexpr int kGu = gu_words(FQ), kDown = OT * 2 * kFragment;
@@ -18,37 +18,32 @@ __global__ void __launch_bounds__(WAVES *kWave, 2) k_ff_kept(FfArgs a) {
   stage<WAVES, kGu>(a.gu, gu);
   const RowAt at = row_at(a, base < a.rows ? base : a.rows - 1, m);
   Split x[FQ];
-  {
-    const float *const row = a.X[at.t] + at.i * a.ldx;
-    float v[FQ][8];
-#pragma unroll
-    for (int q = 0; q < FQ; ++q) load8(v[q], row, q * kDepth + 8 * g, a.F, a.vec_x);
-#pragma unroll
-    for (int q = 0; q < FQ; ++q) x[q] = split8(v[q]);
-  }
+  const float inv_x = load_row(x, a.X[at.t] + at.i * a.ldx, g, a.F, a.vec_x);
   f32x16 y[OT];
 #pragma unroll
   for (int o = 0; o < OT; ++o) y[o] = per_row(a.bd + o * kTile, g);
-  const float *const bias = reinterpret_cast<const float *>(gu + FQ * 2 * kFragment);
   for (int h = 0; h < a.ht; ++h) {
     staged();
     stage<WAVES, kDown>(a.down + (int64_t)h * kDown, down);
-    f32x16 G = per_row(bias, g), U = per_row(bias + kTile, g);
+    Sums sg = no_sums(), su = no_sums();
 #pragma unroll
     for (int q = 0; q < FQ; ++q) {
-      G = product(fragment(gu, 2 * q), x[q], G);
-      U = product(fragment(gu, 2 * q + 1), x[q], U);
+      add_product(sg, fragment(gu, 2 * q), x[q]);
+      add_product(su, fragment(gu, 2 * q + 1), x[q]);
     }
+    const TileVectors &v = vectors_of(gu, FQ);
+    const float inv = inv_x * v.inv_gu, inv_down = v.inv_down;
+    f32x16 G = value_of(sg, inv, v.bg, g);
+    const f32x16 U = value_of(su, inv, v.bu, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
+    const Scale scale = scale_for(max_over_32(largest_of(G)));
+    const Split b[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)};
     staged();
     if (h + 1 < a.ht) stage<WAVES, kGu>(a.gu + (int64_t)(h + 1) * kGu, gu);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const Split b = half(G, s);
-#pragma unroll
-      for (int o = 0; o < OT; ++o) y[o] = product(fragment(down, 2 * o + s), b, y[o]);
-    }
+    for (int o = 0; o < OT; ++o)
+      add(y[o], scale.inv * inv_down, product(fragment(down, 2 * o + 1), b[1], product(fragment(down, 2 * o), b[0], zeros())));
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;

@@ -4,11 +4,11 @@
 // workgroup share the node rows, 32 of one snapshot at a time, whose pieces lie in LDS row by row in two slots, so that one barrier
 // a tile is enough: while a tile is multiplied the next one is split and laid down.  G, U and dH are made with a node row a result row, so that
 // dG, dU and H are operands of products whose depth is the node rows; the other operand, X or dY with its columns along the lanes, comes from
-// the same LDS rows by loads that transpose.
+// the same LDS rows by loads that transpose.  It keeps its rows' scales there, by whose inverses dG, dU and H are multiplied before they get a
+// scale of their own: a lane's, since a lane is a hidden column of theirs and of the result.
 //
 // Everything is in 16 x 16 x 32 instructions: 16 columns a wave rather than 32 halve the registers for weights and gradients, so that two
-// waves share a SIMD (64 columns: 244 registers) and the one's elementwise work, some 1900 cycles a tile, runs beside the other's 2304 of matrix
-// instructions.  With 32 columns and one wave a SIMD it took 3.5 ms on 1.6 million rows of 64 through 256 columns.
+// waves share a SIMD and one's elementwise work runs beside the other's matrix instructions.
 // l = lane % 16, g = lane / 16: an operand's lane holds row (column) l, depth 8 g .. 8 g + 7; register r of the result is row 4 g + r, column l.
 // Two results one below the other are an operand whose depth runs over 16 (j / 4) + 4 g + j % 4; a load that transposes gives lane l of 16 the
 // 16-bit values of column l in four rows, whose 8-byte pieces the lanes 4 j + c address (row j, columns 4 c ..).
@@ -23,56 +23,59 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 __device__ inline f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 __device__ inline f32x4 product16(const Split &a, const Split &b, f32x4 c) {  // as product()
-  c = mfma16(a.p[2], b.p[0], c);
-  c = mfma16(a.p[0], b.p[2], c);
-  c = mfma16(a.p[1], b.p[1], c);
   c = mfma16(a.p[1], b.p[0], c);
   c = mfma16(a.p[0], b.p[1], c);
   return mfma16(a.p[0], b.p[0], c);
 }
 
-// The pieces of 32 rows of 32 D columns: three planes, rows 16 bytes further apart than they are long, so that 16 lanes that read 16 bytes of a
-// row each, or 8 bytes of four rows each, meet all banks once.
+// The pieces of 32 rows of 32 D columns, two planes, and 1 over the rows' scales.  The 16-byte chunks of a row are permuted by its number, so that
+// 16 lanes that read a chunk of a row each, and 32 that read 8 bytes of eight rows, meet all 64 banks once: rows of 64 D bytes are 4 / D to the
+// 256 of all banks, and the chunks of those that lie on the same banks have to differ, for the loads that transpose in pairs.
 template <int D>
 struct Slot {
-  static constexpr int kStride = 64 * D + 16;
-  char plane[3][kTile * kStride];
+  char plane[2][kTile * 64 * D];
+  float inv[kTile];
+  __device__ static int place(int row, int chunk) {
+    const int high = row >> 3 & 1;
+    const int f = D == 1 ? (row >> 2 & 1) * 2 + high : D == 2 ? (row >> 1 & 3) * 2 + high : (row & 7) * 2 + high;
+    return row * 64 * D + ((chunk ^ f) << 4);
+  }
   __device__ void put(int row, int chunk, const Split &s) {  // columns 8 chunk ..
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4 *>(plane[p] + row * kStride + 16 * chunk) = s.p[p];
+    for (int p = 0; p < 2; ++p) *reinterpret_cast<u32x4 *>(plane[p] + place(row, chunk)) = s.p[p];
   }
   // rows 16 sub .., columns 32 d ..
   __device__ Split plain(int sub, int d, int lane) const {
-    const int at = (16 * sub + lane % 16) * kStride + 64 * d + 16 * (lane / 16);
+    const int at = place(16 * sub + lane % 16, 4 * d + lane / 16);
     Split s;
 #pragma unroll
-    for (int p = 0; p < 3; ++p) s.p[p] = *reinterpret_cast<const u32x4 *>(plane[p] + at);
+    for (int p = 0; p < 2; ++p) s.p[p] = *reinterpret_cast<const u32x4 *>(plane[p] + at);
     return s;
   }
   // columns 16 t .., all 32 rows
   __device__ Split transposed(int t, int lane) const {
-    const int at = (4 * (lane / 16) + lane % 16 / 4) * kStride + 32 * t + 8 * (lane % 4);
+    const int row = 4 * (lane / 16) + lane % 16 / 4, c = lane % 4;
+    const int at = place(row, 2 * t + c / 2) + 8 * (c % 2);  // (16 rows further on the chunks lie alike)
     Split s;
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-      typedef const __attribute__((address_space(3))) s16x4 *Lds;
+    for (int p = 0; p < 2; ++p) {
       union {
         s16x4 h[2];
         u32x4 w;
       } both;
 #pragma unroll
       for (int half = 0; half < 2; ++half)
-        both.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(Lds)(plane[p] + at + 16 * half * kStride));
+        both.h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(plane[p] + at + 16 * half * 64 * D));
       s.p[p] = both.w;
     }
     return s;
   }
 };
 
-// A thread's share of the rows that come next: 8 columns at a time, D of them 8 rows apart ... D (32 rows are 128 D pieces of 8 columns).
+// A thread's share of the rows that come next, 8 columns at a time: 4 D consecutive threads have a row.
 template <int D>
 struct Share {
   static constexpr int kMine = kTile * 4 * D / kBlock > 0 ? kTile * 4 * D / kBlock : 1, kChunks = 4 * D;
@@ -84,15 +87,42 @@ struct Share {
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
       const int r = row(q);
-      load8(v[q], first + (r < count ? r : 0) * ld, 8 * chunk(), there() && r < count ? F : 0, vec);
+      const float *const at = first + (r < count ? r : 0) * ld;
+      if (vec && F % 8 == 0) {  // (no column is left out of a piece)
+        float4 t[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+        if (there() && r < count && 8 * chunk() < F) {
+          t[0] = *reinterpret_cast<const float4 *>(at + 8 * chunk());
+          t[1] = *reinterpret_cast<const float4 *>(at + 8 * chunk() + 4);
+        }
+        v[q][0] = t[0].x, v[q][1] = t[0].y, v[q][2] = t[0].z, v[q][3] = t[0].w;
+        v[q][4] = t[1].x, v[q][5] = t[1].y, v[q][6] = t[1].z, v[q][7] = t[1].w;
+      } else {
+        load8(v[q], at, 8 * chunk(), there() && r < count ? F : 0, vec);
+      }
     }
   }
   __device__ void lay_down(Slot<D> &slot, float sign) {
     if (!there()) return;
 #pragma unroll
-    for (int q = 0; q < kMine; ++q) slot.put(row(q), chunk(), split8(v[q], sign));
+    for (int q = 0; q < kMine; ++q) {
+      uint32_t x = __float_as_uint(largest_of(v[q]));  // of a row: its lanes are 4, 8 or 16 neighbours (not negative: floats compare as integers)
+      x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));   // quad_perm: lane ^ 1
+      x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));   // quad_perm: lane ^ 2
+      if (kChunks >= 8) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));   // row_half_mirror: the other four
+      if (kChunks >= 16) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));  // row_mirror: the other eight
+      const Scale scale = scale_for(__uint_as_float(x));
+      slot.put(row(q), chunk(), split8<false>(v[q], sign * scale.to));
+      if (chunk() == 0) slot.inv[row(q)] = scale.inv;
+    }
   }
 };
+
+// A lane's 8 values, a hidden column in four lanes, as pieces; returns 1 over their scale.
+__device__ inline float pieces_of(const float (&v)[8], Split *to) {
+  const Scale scale = scale_for(max_over_32(max_over_16(largest_of(v))));
+  *to = split8<false>(v, scale.to);
+  return scale.inv;
+}
 
 template <int ACT, int FD, int OD>
 __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weights(FfArgs a) {
@@ -103,30 +133,41 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   const bool there = hid < a.hidden;
 
   Split wg[FD], wu[FD], wd[OD];
+  float inv_gu, inv_up;
   {
-    float v[8];
+    float v[2][FD][8], largest = 0.f;
 #pragma unroll
-    for (int q = 0; q < FD; ++q) {
+    for (int w = 0; w < 2; ++w)
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
+      for (int q = 0; q < FD; ++q) {
         const float *const W = w ? a.Wu : a.Wg;
         const int64_t ld = w ? a.ldwu : a.ldwg;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int f = 32 * q + 8 * g + j;
-          v[j] = there && f < a.F ? W[f * ld + hid] : 0.f;
+          v[w][q][j] = there && f < a.F ? W[f * ld + hid] : 0.f;
         }
-        (w ? wu : wg)[q] = split8(v);
+        largest = largest_of(v[w][q], largest);
       }
-    }
+    const Scale scale = scale_for(max_of_wave(largest));
+    inv_gu = scale.inv;
+#pragma unroll
+    for (int q = 0; q < FD; ++q) wg[q] = split8<false>(v[0][q], scale.to), wu[q] = split8<false>(v[1][q], scale.to);
+  }
+  {
+    float v[OD][8], largest = 0.f;
 #pragma unroll
     for (int q = 0; q < OD; ++q) {
-      load8(v, a.Wd + (there ? hid : 0) * a.ldwd, 32 * q + 8 * g, there ? a.Fo : 0, false);
-      wd[q] = split8(v);
+      load8(v[q], a.Wd + (there ? hid : 0) * a.ldwd, 32 * q + 8 * g, there ? a.Fo : 0, false);
+      largest = largest_of(v[q], largest);
     }
+    const Scale scale = scale_for(max_of_wave(largest));
+    inv_up = scale.inv;
+#pragma unroll
+    for (int q = 0; q < OD; ++q) wd[q] = split8<false>(v[q], scale.to);
   }
   const float bg = there && a.bg ? a.bg[hid] : 0.f, bu = there && a.bu ? a.bu[hid] : 0.f;
-  f32x4 dwg[2 * FD], dwu[2 * FD], dwd[2 * OD];
+  f32x4 dwg[2 * FD], dwu[2 * FD], dwd[2 * OD];  // dwd transposed: its rows are Y's columns
 #pragma unroll
   for (int t = 0; t < 2 * FD; ++t) dwg[t] = dwu[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -164,55 +205,63 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   lay_down(0, 1.f);
   load_next();
   __syncthreads();
+  const f32x4 zero{0.f, 0.f, 0.f, 0.f};
   float sign = 1.f;
   for (int64_t i = 0; i < count; ++i) {
     const Slot<FD> &X = xs[i & 1];
     const Slot<OD> &dY = dys[i & 1];
-    f32x4 G[2], U[2], dH[2];
+    f32x4 sg[2], su[2], sd[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const float b = sign * bg, c = sign * bu;
-      G[s] = f32x4{b, b, b, b}, U[s] = f32x4{c, c, c, c}, dH[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+      sg[s] = su[s] = sd[s] = zero;
 #pragma unroll
       for (int q = 0; q < FD; ++q) {
         const Split p = X.plain(s, q, lane);
-        G[s] = product16(p, wg[q], G[s]);
-        U[s] = product16(p, wu[q], U[s]);
+        sg[s] = product16(p, wg[q], sg[s]);
+        su[s] = product16(p, wu[q], su[s]);
       }
 #pragma unroll
-      for (int q = 0; q < OD; ++q) dH[s] = product16(dY.plain(s, q, lane), wd[q], dH[s]);
+      for (int q = 0; q < OD; ++q) sd[s] = product16(dY.plain(s, q, lane), wd[q], sd[s]);
     }
     if (i + 1 < count) {
       lay_down((int)(i + 1) & 1, -sign);
       load_next();
     }
-    // X and dY have this tile's sign, which cancels in the product of dH and U
+    // X and dY have this tile's sign
+    const float sign_gu = sign * inv_gu, sign_up = sign * inv_up;
     float vg[8], vu[8], vh[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float2 c = activate_slope<ACT>(sign * G[j / 4][j % 4]);
-      const float u = U[j / 4][j % 4], d = dH[j / 4][j % 4], as = sign * c.x;
-      vg[j] = d * u * c.y;
-      vu[j] = d * as;
-      vh[j] = as * u;
-      dbg += vg[j];
-      dbu += vu[j];
+    for (int s = 0; s < 2; ++s) {
+      const f32x4 inv_x = *reinterpret_cast<const f32x4 *>(X.inv + 16 * s + 4 * g), inv_dy = *reinterpret_cast<const f32x4 *>(dY.inv + 16 * s + 4 * g);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = 4 * s + r;
+        const float cx = sign_gu * inv_x[r];
+        const float2 c = activate_slope<ACT>(fmaf(sg[s][r], cx, bg));
+        const float u = fmaf(su[s][r], cx, bu), d = sd[s][r] * (sign_up * inv_dy[r]);
+        vg[j] = d * u * c.y;
+        vu[j] = d * c.x;
+        dbg += vg[j];
+        dbu += vu[j];
+        vg[j] *= inv_x[r];
+        vu[j] *= inv_x[r];
+        vh[j] = c.x * u * inv_dy[r];
+      }
     }
-    const Split dg = split8(vg), du = split8(vu), hh = split8(vh);
-    const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+    Split dg, du, hh;
+    const float cg = sign * pieces_of(vg, &dg), cu = sign * pieces_of(vu, &du), ch = sign * pieces_of(vh, &hh);
+    const auto add = [](f32x4 &to, float factor, const f32x4 &x) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) to[r] = fmaf(x[r], factor, to[r]);
+    };
 #pragma unroll
     for (int q = 0; q < 2 * FD; ++q) {
       const Split p = X.transposed(q, lane);
-      const f32x4 gs = product16(p, dg, zero), us = product16(p, du, zero);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) dwg[q][r] = fmaf(sign, gs[r], dwg[q][r]), dwu[q][r] = fmaf(sign, us[r], dwu[q][r]);
+      add(dwg[q], cg, product16(p, dg, zero));
+      add(dwu[q], cu, product16(p, du, zero));
     }
 #pragma unroll
-    for (int q = 0; q < 2 * OD; ++q) {
-      const f32x4 ds = product16(hh, dY.transposed(q, lane), zero);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) dwd[q][r] = fmaf(sign, ds[r], dwd[q][r]);
-    }
+    for (int q = 0; q < 2 * OD; ++q) add(dwd[q], ch, product16(dY.transposed(q, lane), hh, zero));
     __syncthreads();
     sign = -sign;
   }
@@ -247,15 +296,15 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
           to[((int64_t)a.F + f) * a.hidden + hid] = dwu[q][r];
         }
       }
+#pragma unroll
+    for (int q = 0; q < 2 * OD; ++q)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int fo = 16 * q + 4 * g + r;
+        if (fo < a.Fo) to_d[(int64_t)hid * a.Fo + fo] = dwd[q][r];
+      }
     if (g == 0) to_b[hid] = dbg, to_b[a.hidden + hid] = dbu;
   }
-#pragma unroll
-  for (int q = 0; q < 2 * OD; ++q)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int row = hid - l + 4 * g + r, fo = 16 * q + l;
-      if (row < a.hidden && fo < a.Fo) to_d[(int64_t)row * a.Fo + fo] = dwd[q][r];
-    }
 }
 
 template <int ACT, int FD>
