@@ -173,6 +173,17 @@ __device__ inline Split half(const f32x16 &r, int s, float scale) {  // the regi
   return split8<WIDE>(v, scale);
 }
 
+// A sum of many terms that carries what the additions round off (over thousands of tiles a plain one is off by more than 1e-6).
+struct Total {
+  float sum = 0.f, lost = 0.f;
+  __device__ void add(float x) {
+    x -= lost;
+    const float s = sum + x;
+    lost = (s - sum) - x;
+    sum = s;
+  }
+};
+
 // ---- the activations ----------------------------------------------------------------------------
 // The normal distribution's tail Q(|x|) = 1 - Phi(|x|), and its density times sqrt(2 pi), exp(-x^2 / 2).  Q is that times a function that falls like
 // 1 / |x|: a polynomial in k = 1 / (1 + 0.275 |x|) without a constant term, fitted for the least error of |x| Q (1.1e-8, 6.9e-8 with the
@@ -226,7 +237,7 @@ struct FfArgs {
   // back, narrow: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
   const u32x4 *gu, *down, *up, *back;
   const float *bd;  // padded with zeros to whole tiles
-  const float *Wg, *Wu, *Wd, *bg, *bu;  // as they came
+  const float *Wg, *Wu, *Wd, *bg, *bu, *bd_in;  // as they came
   int64_t ldwg, ldwu, ldwd;
   // weight gradients: partial sums of `parts` ranges of rows, each [dWg F x hidden | dWu | dWd hidden x Fo | dbg | dbu | dbd]
   float *partial;

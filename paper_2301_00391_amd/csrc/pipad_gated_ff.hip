@@ -152,6 +152,64 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
   for (int o = 0; o < OT; ++o) store_tile(y[o], out, (o0 + o) * kTile, a.Fo, a.vec_o, g);
 }
 
+// Few rows: a workgroup a row, in 32-bit floats, straight from the weights as they are.  What counts is the time from the first load to the last
+// store: no launch for fragments, and every wave has its loads on the way at once.  Columns lie along the lanes; the sum over the rows
+// of a matrix is shared by as many waves as there are left, and added up in LDS, always in the same order.
+constexpr int kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewColumns = 1024, kFewMostF = 2048;
+// part[group][column] over LDS: the waves of `blocks` blocks of 64 columns, `groups` waves for each.
+template <int ACT>
+__global__ void __launch_bounds__(kFewThreads) k_ff_few(FfArgs a) {
+  __shared__ float x[kFewMostF], sum_g[kFewThreads], sum_u[kFewThreads], hidden[kFewColumns];
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const RowAt at = row_at(a, blockIdx.x, 0);
+  const float *const row = a.X[at.t] + at.i * a.ldx;
+  for (int f = threadIdx.x; f < a.F; f += kFewThreads) x[f] = row[f];
+  float *const out = a.out[at.t] + at.i * a.ldo;
+  __syncthreads();
+  for (int h0 = 0; h0 < a.hidden; h0 += kFewColumns) {
+    const int columns = min(a.hidden - h0, kFewColumns), blocks = (columns + kWave - 1) / kWave, groups = kFewWaves / blocks;
+    {
+      const int group = wave / blocks, c = wave % blocks * kWave + lane;
+      float g = 0.f, u = 0.f;
+      if (group < groups && c < columns) {
+        const float *const wg = a.Wg + h0 + c, *const wu = a.Wu + h0 + c;
+#pragma unroll 16
+        for (int f = group; f < a.F; f += groups) {
+          g = fmaf(x[f], wg[f * a.ldwg], g);
+          u = fmaf(x[f], wu[f * a.ldwu], u);
+        }
+      }
+      sum_g[threadIdx.x] = g, sum_u[threadIdx.x] = u;
+    }
+    __syncthreads();
+    if (threadIdx.x < columns) {
+      float g = a.bg ? a.bg[h0 + threadIdx.x] : 0.f, u = a.bu ? a.bu[h0 + threadIdx.x] : 0.f;
+      for (int q = 0; q < groups; ++q) g += sum_g[q * blocks * kWave + threadIdx.x], u += sum_u[q * blocks * kWave + threadIdx.x];
+      hidden[threadIdx.x] = activate<ACT>(g) * u;
+    }
+    __syncthreads();
+    for (int o0 = 0; o0 < a.Fo; o0 += kFewColumns) {
+      const int outs = min(a.Fo - o0, kFewColumns), oblocks = (outs + kWave - 1) / kWave, ogroups = kFewWaves / oblocks;
+      const int group = wave / oblocks, c = wave % oblocks * kWave + lane;
+      float y = 0.f;
+      if (group < ogroups && c < outs) {
+        const float *const wd = a.Wd + h0 * a.ldwd + o0 + c;
+#pragma unroll 16
+        for (int h = group; h < columns; h += ogroups) y = fmaf(hidden[h], wd[h * a.ldwd], y);
+      }
+      sum_g[threadIdx.x] = y;
+      __syncthreads();
+      if (threadIdx.x < outs) {
+        const int o = o0 + threadIdx.x;
+        float s = h0 ? out[o] : a.bd_in ? a.bd_in[o] : 0.f;
+        for (int q = 0; q < ogroups; ++q) s += sum_g[q * oblocks * kWave + threadIdx.x];
+        out[o] = s;
+      }
+      __syncthreads();
+    }
+  }
+}
+
 // ---- the gradient of X --------------------------------------------------------------------------
 template <int ACT, int FT>
 __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
@@ -222,7 +280,7 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
   f32x16 dwg[T], dwu[T], dwd[T];  // dwd transposed: its rows are Y's columns
 #pragma unroll
   for (int t = 0; t < T; ++t) dwg[t] = dwu[t] = dwd[t] = zeros();
-  float dbg = 0.f, dbu = 0.f, dbd[T] = {};
+  Total dbg, dbu, dbd[T];
   const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
   const TileVectors &vectors = vectors_of(gu, a.fq);
   const float bg = vectors.bg[m], bu = vectors.bu[m];
@@ -246,7 +304,7 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
       load8(v, dy, q * kDepth + 8 * g, there ? a.Fo : 0, a.vec_dy);
       add_product(sd, split8<true>(v, sign * scale_dy.to), fragment(a.up, (int64_t)h * a.oq + q));
     }
-    float vg[16], vu[16], vh[16], to_x[16], to_dy[16];
+    float vg[16], vu[16], vh[16], to_x[16], to_dy[16], tile_g = 0.f, tile_u = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int d = result_depth(r / 8, g, r % 8);
@@ -257,12 +315,13 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
       const float u = fmaf(su.main[r], cx, fmaf(su.cross[r], cx * (1.f / kWide), bu)), e = fmaf(sd.main[r], cd, sd.cross[r] * (cd * (1.f / kWide)));
       vg[r] = e * u * c.y;
       vu[r] = e * c.x;
-      dbg += vg[r];
-      dbu += vu[r];
+      tile_g += vg[r];
+      tile_u += vu[r];
       vg[r] *= inv_x;
       vu[r] *= inv_x;
       vh[r] = c.x * u * inv_dy;
     }
+    dbg.add(tile_g), dbu.add(tile_u);
     const auto pieces = [&](const float (&from)[16], Split (&to)[2]) {
       const Scale scale = scale_for(max_over_32(largest_of(from)));
 #pragma unroll
@@ -311,7 +370,7 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
         for (int s = 0; s < 2; ++s) {
           const Split ds = transposed(a.dY, a.lddy, a.Fo, to_dy, s);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) dbd[t] += v[j];
+          for (int j = 0; j < 8; ++j) dbd[t].add(v[j]);
           add_product(d_sum, ds, hh[s]);
         }
         add_sums(dwd[t], ch, d_sum);
@@ -332,15 +391,14 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
       if (c < a.Fo && hid < a.hidden) to_d[(int64_t)hid * a.Fo + c] = dwd[t][r];
     }
   float *const to_b = to_d + (int64_t)a.hidden * a.Fo;
-  dbg += __shfl_xor(dbg, 32);
-  dbu += __shfl_xor(dbu, 32);
+  const float sum_g = dbg.sum + __shfl_xor(dbg.sum, 32), sum_u = dbu.sum + __shfl_xor(dbu.sum, 32);
   if (blockIdx.z == 0 && g == 0 && hid < a.hidden) {
-    to_b[hid] = dbg;
-    to_b[a.hidden + hid] = dbu;
+    to_b[hid] = sum_g;
+    to_b[a.hidden + hid] = sum_u;
   }
 #pragma unroll
   for (int t = 0; t < T; ++t) {
-    const float b = dbd[t] + __shfl_xor(dbd[t], 32);
+    const float b = dbd[t].sum + __shfl_xor(dbd[t].sum, 32);
     const int fo = (t0 + t) * kTile + m;
     if (h == 0 && g == 0 && fo < a.Fo) to_b[2 * a.hidden + fo] = b;
   }
@@ -404,7 +462,7 @@ struct Plan {
   int64_t n_gu, n_down, n_up, n_back;
   size_t gu, down, up, back, bd, partial, total;
   int64_t rows, part_floats, parts, tiles_per_part;
-  bool kept;
+  bool kept, few;
   Plan(const pipad_gated_ff_t &c, int32_t n, int32_t k, bool backward) {
     ht = (int32_t)tiles(c.hidden, kTile);
     fq = depth_tiles(c.F, backward), ft = column_tiles(c.F), oq = depth_tiles(c.Fo, backward), ot = column_tiles(c.Fo);
@@ -432,6 +490,10 @@ struct Plan {
     const int64_t most = std::max<int64_t>(1, kept ? at_a_time / tiles(c.hidden, 16 * kWavesPerBlock) : 2048 / ht);
     tiles_per_part = std::max<int64_t>(4, tiles(row_tiles, most));
     parts = tiles(row_tiles, tiles_per_part);
+    // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
+    // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; in tiles of rows 16.7 to 18.3 throughout (32 through 128: 5.9, 6.5, 11.5 and 9.4 to 10.3).
+    // Rows of more than 128 columns, 256 through 1024: 47.5, 50.3, 96.9 and 381 at 2048; in tiles 493 to 564.
+    few = !backward && rows <= (kept ? 256 : 2048) && c.F <= kFewMostF;
     partial = take(backward ? (size_t)parts * part_floats * sizeof(float) : 0);
     total = at;
   }
@@ -452,7 +514,7 @@ FfArgs arguments(const pipad_gated_ff_t &c, const Plan &p, int32_t n, int32_t k,
   a.gu = reinterpret_cast<const u32x4 *>(ws + p.gu), a.down = reinterpret_cast<const u32x4 *>(ws + p.down);
   a.up = reinterpret_cast<const u32x4 *>(ws + p.up), a.back = reinterpret_cast<const u32x4 *>(ws + p.back);
   a.bd = reinterpret_cast<const float *>(ws + p.bd);
-  a.Wg = c.Wg, a.Wu = c.Wu, a.Wd = c.Wd, a.bg = c.bg, a.bu = c.bu, a.ldwg = c.ldwg, a.ldwu = c.ldwu, a.ldwd = c.ldwd;
+  a.Wg = c.Wg, a.Wu = c.Wu, a.Wd = c.Wd, a.bg = c.bg, a.bu = c.bu, a.bd_in = c.bd, a.ldwg = c.ldwg, a.ldwu = c.ldwu, a.ldwd = c.ldwd;
   a.partial = reinterpret_cast<float *>(ws + p.partial), a.part_floats = p.part_floats, a.tiles_per_part = p.tiles_per_part;
   return a;
 }
@@ -472,6 +534,7 @@ using FfKernel = void (*)(FfArgs);
 #define PIPAD_FF_KERNELS(name, ...) \
   constexpr FfKernel name##_of[4][3] = {{name<0, 1>, name<0, 2>, name<0, __VA_ARGS__>}, {name<1, 1>, name<1, 2>, name<1, __VA_ARGS__>}, \
                                         {name<2, 1>, name<2, 2>, name<2, __VA_ARGS__>}, {name<3, 1>, name<3, 2>, name<3, __VA_ARGS__>}};
+constexpr FfKernel k_ff_few_of[4] = {k_ff_few<0>, k_ff_few<1>, k_ff_few<2>, k_ff_few<3>};
 PIPAD_FF_KERNELS(k_ff_rows, 4)
 PIPAD_FF_KERNELS(k_ff_rows_backward, 4)
 PIPAD_FF_KERNELS(k_ff_weights_backward, 2)
@@ -487,9 +550,14 @@ int gated_ff_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float
                     void *workspace, hipStream_t st) {
   const Plan p(c, n, k, false);
   char *const ws = static_cast<char *>(workspace);
+  const FfArgs a = arguments(c, p, n, k, X, ldx, nullptr, 0, Y, ldy, ws);
+  if (p.few) {
+    hipLaunchKernelGGL(k_ff_few_of[c.activation], dim3((unsigned)p.rows), dim3(kFewThreads), 0, st, a);
+    PIPAD_HIP(hipGetLastError());
+    return PIPAD_OK;
+  }
   const int rc = pack(c, p, ws, st);
   if (rc != PIPAD_OK) return rc;
-  const FfArgs a = arguments(c, p, n, k, X, ldx, nullptr, 0, Y, ldy, ws);
   if (p.kept) {
     const Kept f = kept_forward(c.activation, p.fq, p.ot);
     hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, kTile * f.waves)), dim3(f.waves * kWave), 0, st, a);

@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   for (int t = 0; t < 2 * FD; ++t) dwg[t] = dwu[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int t = 0; t < 2 * OD; ++t) dwd[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float dbg = 0.f, dbu = 0.f, dbd[8] = {};
+  Total dbg, dbu, dbd[8];
 
   // the part's tiles, of each snapshot a whole number, and the place of the one that is loaded next
   const int64_t of_snapshot = ((int64_t)a.n + kTile - 1) / kTile, every = of_snapshot * a.k;
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
 #pragma unroll
       for (int q = 0; q < Share<OD>::kMine; ++q)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dbd[j] += dy.v[q][j];
+        for (int j = 0; j < 8; ++j) dbd[j].add(dy.v[q][j]);
     dy.lay_down(dys[slot], sign);
   };
 
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
     }
     // X and dY have this tile's sign
     const float sign_gu = sign * inv_gu, sign_up = sign * inv_up;
-    float vg[8], vu[8], vh[8];
+    float vg[8], vu[8], vh[8], tile_g = 0.f, tile_u = 0.f;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const f32x4 inv_x = *reinterpret_cast<const f32x4 *>(X.inv + 16 * s + 4 * g), inv_dy = *reinterpret_cast<const f32x4 *>(dY.inv + 16 * s + 4 * g);
@@ -241,13 +241,14 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
         const float u = fmaf(su[s][r], cx, bu), d = sd[s][r] * (sign_up * inv_dy[r]);
         vg[j] = d * u * c.y;
         vu[j] = d * c.x;
-        dbg += vg[j];
-        dbu += vu[j];
+        tile_g += vg[j];
+        tile_u += vu[j];
         vg[j] *= inv_x[r];
         vu[j] *= inv_x[r];
         vh[j] = c.x * u * inv_dy[r];
       }
     }
+    dbg.add(tile_g), dbu.add(tile_u);
     Split dg, du, hh;
     const float cg = sign * pieces_of(vg, &dg), cu = sign * pieces_of(vu, &du), ch = sign * pieces_of(vh, &hh);
     const auto add = [](f32x4 &to, float factor, const f32x4 &x) {
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
     constexpr int kThreads = kBlock / Share<OD>::kChunks;  // threads of a chunk of columns
     if (Share<OD>::there())
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sums[(threadIdx.x / Share<OD>::kChunks) * 32 * OD + 8 * Share<OD>::chunk() + j] = dbd[j];
+      for (int j = 0; j < 8; ++j) sums[(threadIdx.x / Share<OD>::kChunks) * 32 * OD + 8 * Share<OD>::chunk() + j] = dbd[j].sum;
     __syncthreads();
     for (int c = threadIdx.x; c < a.Fo; c += kBlock) {
       float s = 0.f;
@@ -281,10 +282,11 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
     }
   }
   // (all lanes have to take part before those without a column leave)
-  dbg += __shfl_xor(dbg, 16);
-  dbu += __shfl_xor(dbu, 16);
-  dbg += __shfl_xor(dbg, 32);
-  dbu += __shfl_xor(dbu, 32);
+  const auto over_rows = [](float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+  };
+  const float sum_g = over_rows(dbg.sum), sum_u = over_rows(dbu.sum);
   if (there) {
 #pragma unroll
     for (int q = 0; q < 2 * FD; ++q)
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
         const int fo = 16 * q + 4 * g + r;
         if (fo < a.Fo) to_d[(int64_t)hid * a.Fo + fo] = dwd[q][r];
       }
-    if (g == 0) to_b[hid] = dbg, to_b[a.hidden + hid] = dbu;
+    if (g == 0) to_b[hid] = sum_g, to_b[a.hidden + hid] = sum_u;
   }
 }
 

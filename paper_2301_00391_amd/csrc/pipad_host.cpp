@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
 #include <c10/core/Allocator.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -348,7 +349,238 @@ PyObject *update(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
   });
 }
 
+// ---- operators on node rows ----------------------------------------------------------------------
+// The operands of one call: the first says how many rows and matrices there are and where, all others go with it.
+struct RowsCall {
+  int64_t n = 0, k = 0;
+  long device = -1;
+  bool first(PyObject *o, long current, Matrices *m) {
+    Items list;
+    const at::Tensor *t = nullptr;
+    if (items(o, &list)) {
+      if (list.count < 1 || list.count > PIPAD_MAX_K || !(t = plain_tensor(list.at[0])) || t->dim() != 2) return false;
+      n = t->size(0), k = list.count;
+    } else {
+      if (!(t = plain_tensor(o)) || t->dim() != 3 || t->size(1) < 1 || t->size(1) > PIPAD_MAX_K) return false;
+      n = t->size(0), k = t->size(1);
+    }
+    device = t->get_device();
+    return device == current && n <= INT32_MAX && rows(o, m) && m->F >= 1 && m->F <= INT32_MAX;
+  }
+  bool here(PyObject *o) const {  // (a plain tensor)
+    return THPVariable_Unpack(o).get_device() == device;
+  }
+  bool rows(PyObject *o, Matrices *m) const {
+    if (!operand(o, n, k, m)) return false;
+    Items list;
+    if (!items(o, &list)) return here(o);
+    for (Py_ssize_t t = 0; t < list.count; ++t)
+      if (!here(list.at[t])) return false;
+    return true;
+  }
+  bool rows_or_none(PyObject *o, int64_t F, Matrices *m, bool *there) const {
+    *there = o != Py_None;
+    m->ld = 0;
+    return !*there || (rows(o, m) && m->F == F);
+  }
+  bool vector(PyObject *o, int64_t F, const float **at) const {
+    *at = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *t = plain_tensor(o);
+    if (!t || t->scalar_type() != at::kFloat || t->dim() != 1 || t->size(0) != F || (F > 1 && t->stride(0) != 1) || !here(o)) return false;
+    *at = static_cast<const float *>(t->data_ptr());
+    return true;
+  }
+  bool weights(PyObject *o, int64_t rows, int64_t columns, const float **at, int64_t *ld) const {
+    const at::Tensor *t = plain_tensor(o);
+    if (!t || t->scalar_type() != at::kFloat || t->dim() != 2 || t->size(0) != rows || t->size(1) != columns || (columns > 1 && t->stride(1) != 1) || !here(o))
+      return false;
+    *at = static_cast<const float *>(t->data_ptr());
+    *ld = rows > 1 ? t->stride(0) : std::max(columns, t->stride(0));
+    return true;
+  }
+  // The memory that a call needs for itself, which goes back in the order of the current stream: that of the call.
+  static c10::DataPtr memory(size_t bytes) {
+    return bytes ? c10::GetAllocator(c10::DeviceType::CUDA)->allocate(bytes) : c10::DataPtr();
+  }
+  at::Tensor empty(at::IntArrayRef shape) const { return at::empty(shape, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, (c10::DeviceIndex)device)); }
+};
+
+// Wg, Wu, Wd, bg, bu, bd and the activation as a pipad_gated_ff_t
+bool ff_block(const RowsCall &call, PyObject *const *args, int64_t F, long activation, pipad_gated_ff_t *b) {
+  const at::Tensor *g = plain_tensor(args[0]), *d = plain_tensor(args[2]);
+  if (!g || !d || g->dim() != 2 || d->dim() != 2) return false;
+  const int64_t hidden = g->size(1), Fo = d->size(1);
+  if (hidden < 1 || hidden > INT32_MAX || Fo < 1 || Fo > INT32_MAX) return false;
+  b->F = (int32_t)F, b->hidden = (int32_t)hidden, b->Fo = (int32_t)Fo, b->activation = (int32_t)activation;
+  return call.weights(args[0], F, hidden, &b->Wg, &b->ldwg) && call.weights(args[1], F, hidden, &b->Wu, &b->ldwu) &&
+         call.weights(args[2], hidden, Fo, &b->Wd, &b->ldwd) && call.vector(args[3], hidden, &b->bg) && call.vector(args[4], hidden, &b->bu) &&
+         call.vector(args[5], Fo, &b->bd);
+}
+
+// gated_ff(address, address of the size query, current device, stream, X, Wg, Wu, Wd, bg, bu, bd, activation, Y) -> status
+PyObject *gated_ff(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  if (nargs != 13) return PyErr_Format(PyExc_TypeError, "gated_ff: thirteen arguments");
+  return guarded([&]() -> PyObject * {
+    const auto fn = address<decltype(&pipad_gated_ff)>(args[0]);
+    const auto size = address<decltype(&pipad_gated_ff_workspace)>(args[1]);
+    const long current = PyLong_AsLong(args[2]), activation = PyLong_AsLong(args[11]);
+    void *const stream = PyLong_AsVoidPtr(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    RowsCall call;
+    Matrices x, y;
+    pipad_gated_ff_t block;
+    if (!call.first(args[4], current, &x) || !ff_block(call, args + 5, x.F, activation, &block) || !call.rows(args[12], &y) || y.F != block.Fo)
+      Py_RETURN_NONE;
+    size_t bytes = 0;
+    int status = size(&block, (int32_t)call.n, (int32_t)call.k, 0, &bytes);
+    if (status == PIPAD_OK) {
+      const c10::DataPtr memory = RowsCall::memory(bytes);
+      status = unlocked([&] { return fn(&block, (int32_t)call.n, (int32_t)call.k, x.ptr, x.ld, y.ptr, y.ld, memory.get(), bytes, stream); });
+    }
+    return PyLong_FromLong(status);
+  });
+}
+
+// gated_ff_backward(address, address of the size query, current device, stream, X, Wg, Wu, Wd, bg, bu, None, activation, dY, dX or None, weights,
+// biases) -> (status, dWg, dWu, dWd, dbg, dbu, dbd)
+PyObject *gated_ff_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  if (nargs != 16) return PyErr_Format(PyExc_TypeError, "gated_ff_backward: sixteen arguments");
+  return guarded([&]() -> PyObject * {
+    const auto fn = address<decltype(&pipad_gated_ff_backward)>(args[0]);
+    const auto size = address<decltype(&pipad_gated_ff_workspace)>(args[1]);
+    const long current = PyLong_AsLong(args[2]), activation = PyLong_AsLong(args[11]);
+    void *const stream = PyLong_AsVoidPtr(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    const bool weights = args[14] == Py_True, biases = args[15] == Py_True;
+    RowsCall call;
+    Matrices x, dy, dx;
+    pipad_gated_ff_t block;
+    bool want_dx;
+    if (!call.first(args[4], current, &x) || !ff_block(call, args + 5, x.F, activation, &block) || !call.rows(args[12], &dy) || dy.F != block.Fo ||
+        !call.rows_or_none(args[13], x.F, &dx, &want_dx))
+      Py_RETURN_NONE;
+    at::Tensor made[6];
+    pipad_gated_ff_grads_t grads{};
+    if (weights) {
+      made[0] = call.empty({block.F, block.hidden}), made[1] = call.empty({block.F, block.hidden}), made[2] = call.empty({block.hidden, block.Fo});
+      grads.dWg = made[0].data_ptr<float>(), grads.dWu = made[1].data_ptr<float>(), grads.dWd = made[2].data_ptr<float>();
+      grads.lddwg = grads.lddwu = block.hidden, grads.lddwd = block.Fo;
+    }
+    if (biases) {
+      made[3] = call.empty({block.hidden}), made[4] = call.empty({block.hidden}), made[5] = call.empty({block.Fo});
+      grads.dbg = made[3].data_ptr<float>(), grads.dbu = made[4].data_ptr<float>(), grads.dbd = made[5].data_ptr<float>();
+    }
+    size_t bytes = 0;
+    int status = size(&block, (int32_t)call.n, (int32_t)call.k, 1, &bytes);
+    if (status == PIPAD_OK) {
+      const c10::DataPtr memory = RowsCall::memory(bytes);
+      status = unlocked([&] {
+        return fn(&block, (int32_t)call.n, (int32_t)call.k, x.ptr, x.ld, dy.ptr, dy.ld, want_dx ? dx.ptr : nullptr, dx.ld,
+                  weights || biases ? &grads : nullptr, memory.get(), bytes, stream);
+      });
+    }
+    PyObject *const out = PyTuple_New(7);
+    if (!out) return nullptr;
+    PyTuple_SET_ITEM(out, 0, PyLong_FromLong(status));
+    for (int q = 0; q < 6; ++q) {
+      if (!made[q].defined()) Py_INCREF(Py_None);
+      PyTuple_SET_ITEM(out, 1 + q, made[q].defined() ? THPVariable_Wrap(std::move(made[q])) : Py_None);
+    }
+    return out;
+  });
+}
+
+// post, pre, eps, scale, w_post, b_post, w_pre, b_pre as a pipad_residual_norm_t
+bool norm_params(const RowsCall &call, PyObject *const *args, int64_t F, pipad_residual_norm_t *c) {
+  c->F = (int32_t)F, c->post = (int32_t)PyLong_AsLong(args[0]), c->pre = (int32_t)PyLong_AsLong(args[1]), c->eps = (float)PyFloat_AsDouble(args[2]);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  return call.vector(args[3], F, &c->scale) && call.vector(args[4], F, &c->w_post) && call.vector(args[5], F, &c->b_post) &&
+         call.vector(args[6], F, &c->w_pre) && call.vector(args[7], F, &c->b_pre);
+}
+
+// residual_norm(address, current device, stream, R, B, gate, post, pre, eps, scale, w_post, b_post, w_pre, b_pre, R_out, Z) -> status
+PyObject *residual_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  if (nargs != 16) return PyErr_Format(PyExc_TypeError, "residual_norm: sixteen arguments");
+  return guarded([&]() -> PyObject * {
+    const auto fn = address<decltype(&pipad_residual_norm)>(args[0]);
+    const long current = PyLong_AsLong(args[1]);
+    void *const stream = PyLong_AsVoidPtr(args[2]);
+    if (PyErr_Occurred()) return nullptr;
+    RowsCall call;
+    Matrices r, m[4];
+    bool there[4];
+    pipad_residual_norm_t norm;
+    PyObject *const others[4] = {args[4], args[5], args[14], args[15]};
+    if (!call.first(args[3], current, &r) || !norm_params(call, args + 6, r.F, &norm)) Py_RETURN_NONE;
+    for (int q = 0; q < 4; ++q)
+      if (!call.rows_or_none(others[q], r.F, &m[q], &there[q])) Py_RETURN_NONE;
+    const auto at = [&](int q) { return there[q] ? m[q].ptr : nullptr; };
+    const int status = unlocked([&] {
+      return fn(&norm, (int32_t)call.n, (int32_t)call.k, r.ptr, r.ld, at(0), m[0].ld, at(1), m[1].ld, at(2), m[2].ld, at(3), m[3].ld, stream);
+    });
+    return PyLong_FromLong(status);
+  });
+}
+
+// residual_norm_backward(address, address of the size query, current device, stream, R, dR_out, dZ, B, gate, post, pre, eps, scale, w_post, b_post,
+// w_pre, None, dR, dB, dgate, vectors wanted: five truth values) -> (status, dscale, dw_post, db_post, dw_pre, db_pre)
+PyObject *residual_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+  if (nargs != 25) return PyErr_Format(PyExc_TypeError, "residual_norm_backward: twenty-five arguments");
+  return guarded([&]() -> PyObject * {
+    const auto fn = address<decltype(&pipad_residual_norm_backward)>(args[0]);
+    const auto size = address<decltype(&pipad_residual_norm_workspace)>(args[1]);
+    const long current = PyLong_AsLong(args[2]);
+    void *const stream = PyLong_AsVoidPtr(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    RowsCall call;
+    Matrices r, m[7];
+    bool there[7];
+    pipad_residual_norm_t norm;
+    PyObject *const others[7] = {args[7], args[8], args[5], args[6], args[17], args[18], args[19]};  // B, gate, dR_out, dZ, dR, dB, dgate
+    if (!call.first(args[4], current, &r) || !norm_params(call, args + 9, r.F, &norm)) Py_RETURN_NONE;
+    for (int q = 0; q < 7; ++q)
+      if (!call.rows_or_none(others[q], r.F, &m[q], &there[q])) Py_RETURN_NONE;
+    at::Tensor made[5];
+    float *to[5] = {};
+    bool any = false;
+    for (int q = 0; q < 5; ++q)
+      if (args[20 + q] == Py_True) {
+        made[q] = call.empty({r.F});
+        to[q] = made[q].data_ptr<float>();
+        any = true;
+      }
+    const pipad_residual_norm_grads_t grads{to[0], to[1], to[2], to[3], to[4]};
+    size_t bytes = 0;
+    int status = any ? size(norm.F, (int32_t)call.n, (int32_t)call.k, &bytes) : PIPAD_OK;
+    if (status == PIPAD_OK) {
+      const c10::DataPtr memory = RowsCall::memory(bytes);
+      const auto at = [&](int q) { return there[q] ? m[q].ptr : nullptr; };
+      status = unlocked([&] {
+        return fn(&norm, (int32_t)call.n, (int32_t)call.k, r.ptr, r.ld, at(0), m[0].ld, at(1), m[1].ld, at(2), m[2].ld, at(3), m[3].ld, at(4), m[4].ld,
+                  at(5), m[5].ld, at(6), m[6].ld, any ? &grads : nullptr, memory.get(), bytes, stream);
+      });
+    }
+    PyObject *const out = PyTuple_New(6);
+    if (!out) return nullptr;
+    PyTuple_SET_ITEM(out, 0, PyLong_FromLong(status));
+    for (int q = 0; q < 5; ++q) {
+      if (!made[q].defined()) Py_INCREF(Py_None);
+      PyTuple_SET_ITEM(out, 1 + q, made[q].defined() ? THPVariable_Wrap(std::move(made[q])) : Py_None);
+    }
+    return out;
+  });
+}
+
 PyMethodDef methods[] = {
+    {"gated_ff", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(gated_ff)), METH_FASTCALL, "pipad_gated_ff"},
+    {"gated_ff_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(gated_ff_backward)), METH_FASTCALL, "pipad_gated_ff_backward"},
+    {"residual_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(residual_norm)), METH_FASTCALL, "pipad_residual_norm"},
+    {"residual_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(residual_norm_backward)), METH_FASTCALL,
+     "pipad_residual_norm_backward"},
     {"build", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(build)), METH_FASTCALL, "pipad_frame_build_overlap"},
     {"transpose", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(transpose)), METH_FASTCALL, "pipad_frame_transpose"},
     {"aggregate", reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(aggregate)), METH_FASTCALL, "pipad_frame_aggregate or its static form"},

@@ -6,7 +6,8 @@ contract is in ``include/pipad.h``:
 
 Matrices are given as for :func:`frame_aggregate`: a list of k float32 [n, F] matrices that share a row stride, or one [n, k, F]
 tensor.  Results that are not given are allocated in the form of the first operand, a list's k matrices as one piece of memory.
-Calls only enqueue work on the stream.  The workspace comes from PyTorch's allocator where none is given.
+Calls only enqueue work on the stream.  Plain calls with memory for their results go through the binding's native half (see
+binding.py), which leaves anything else to the code here.  The workspace comes from PyTorch's allocator where none is given.
 """
 from __future__ import annotations
 
@@ -16,7 +17,8 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from .binding import MAX_K, Features, _check, _current_raw_stream, _on_device, _operand, _pack_pointers, load_library
+from . import binding
+from .binding import MAX_K, Features, _address, _check, _current_device, _current_raw_stream, _on_device, _operand, _pack_pointers, load_library
 
 _NORMS = {None: 0, "rms": 1, "layer": 2}
 _ACTIVATIONS = {"sigmoid": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -98,11 +100,26 @@ class _Rows:
         return made, made.data_ptr(), nbytes
 
 
-def _choice(table, key, name):
+def _native(results):
+    """(the native half, the current device, its stream) for a call on the current stream that brings the memory of its results."""
+    if binding._host is None or any(r is None for r in results):
+        return None
+    device = _current_device()
+    return binding._host, device, _current_raw_stream(device)
+
+
+def _code(table, key):
     try:
-        return table[key]
-    except (KeyError, TypeError):
-        raise ValueError(f"{name} must be one of {list(table)}") from None
+        return table.get(key)
+    except TypeError:  # nothing that a table could have
+        return None
+
+
+def _choice(table, key, name):
+    code = _code(table, key)
+    if code is None:
+        raise ValueError(f"{name} must be one of {list(table)}")
+    return code
 
 
 # ---- norms ------------------------------------------------------------------------------------------------------------
@@ -133,6 +150,16 @@ def residual_norm(R: Features, B: Optional[Features] = None, gate: Optional[Feat
     returns (R_out, Z).  ``post`` and ``pre`` are "rms", "layer" or None.  Without B, R_out is R and only Z is made; with
     ``pre=None`` there is no Z.  ``R_out`` may be ``R`` itself: the residual stream updated in place."""
     lib = load_library()
+    native = _native((R_out,) * (B is not None) + (Z,) * (pre is not None)) if stream is None else None
+    codes = _code(_NORMS, post), _code(_NORMS, pre)
+    if native is not None and None not in codes:
+        host, device, raw = native
+        status = host.residual_norm(_address["pipad_residual_norm"], device, raw, R, B, gate, *codes, eps, scale, w_post, b_post, w_pre,
+                                    b_pre, R_out, Z)
+        if status is not None:
+            if status:
+                _check(status)
+            return (R if B is None else R_out), Z
     rows = _Rows(R, "R")
     F = rows.width(R)
     r = rows.operand(R, "R")
@@ -156,6 +183,18 @@ def residual_norm_backward(R: Features, dR_out: Optional[Features] = None, dZ: O
     may be None) those of R, B, gate and, unless ``vectors=False``, of the shared vectors: scale, the norms' weights and, unless
     ``biases=False``, their biases.  ``dR`` may be ``dR_out`` itself."""
     lib = load_library()
+    wanted = (B is not None, post is not None, post is not None and biases, pre is not None, pre is not None and biases)
+    wanted = tuple(bool(vectors and w) for w in wanted)
+    native = _native((dR,) + (dB,) * (B is not None) + (dgate,) * (gate is not None)) if stream is None and workspace is None else None
+    codes = _code(_NORMS, post), _code(_NORMS, pre)
+    if native is not None and None not in codes:
+        host, device, raw = native
+        made = host.residual_norm_backward(_address["pipad_residual_norm_backward"], _address["pipad_residual_norm_workspace"], device, raw, R, dR_out, dZ,
+                                           B, gate, *codes, eps, scale, w_post, b_post, w_pre, None, dR, dB, dgate, *wanted)
+        if made is not None:
+            if made[0]:
+                _check(made[0])
+            return ResidualNormGrads(dR, dB, dgate, *made[1:])
     rows = _Rows(R, "R")
     F = rows.width(R)
     r = rows.operand(R, "R")
@@ -166,10 +205,9 @@ def residual_norm_backward(R: Features, dR_out: Optional[Features] = None, dZ: O
         dB = rows.room(F)
     if gate is not None and dgate is None:
         dgate = rows.room(F)
-    wanted = (B is not None, post is not None, post is not None and biases, pre is not None, pre is not None and biases)
-    grads = [torch.empty(F, dtype=torch.float32, device=rows.device) if vectors and w else None for w in wanted]
+    grads = [torch.empty(F, dtype=torch.float32, device=rows.device) if w else None for w in wanted]
     packed, kept, ws = None, None, (0, 0)
-    if vectors:
+    if any(wanted):
         packed = _pack_norm_grads(*[0 if d is None else d.data_ptr() for d in grads])
         need = _size_t()
         _check(lib.pipad_residual_norm_workspace(F, rows.n, rows.k, ctypes.byref(need)))
@@ -210,6 +248,16 @@ def gated_ff(X: Features, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, 
     """pipad_gated_ff: Y = (act(X Wg + bg) * (X Wu + bu)) Wd + bd on the rows of all snapshots, whatever lies between staying on the
     chip.  Wg and Wu are float32 [F, hidden], Wd [hidden, Fo]; ``activation`` is "silu", "gelu" (the exact one), "relu" or "sigmoid"."""
     lib = load_library()
+    native = _native((Y,)) if stream is None and workspace is None else None
+    code = _code(_ACTIVATIONS, activation)
+    if native is not None and code is not None:
+        host, device, raw = native
+        status = host.gated_ff(_address["pipad_gated_ff"], _address["pipad_gated_ff_workspace"], device, raw, X, Wg, Wu, Wd, bg, bu, bd,
+                               code, Y)
+        if status is not None:
+            if status:
+                _check(status)
+            return Y
     rows = _Rows(X, "X")
     F = rows.width(X)
     x = rows.operand(X, "X")
@@ -230,12 +278,24 @@ def gated_ff_backward(X: Features, dY: Features, Wg: torch.Tensor, Wu: torch.Ten
     """pipad_gated_ff_backward: from X and dY the gradient of X (unless ``rows_grad=False``), of the matrices (unless ``weights=False``) and
     of the biases (unless ``biases=False``); G, U and H are made again, so nothing has to be kept from the forward call."""
     lib = load_library()
+    native = _native((dX,) * bool(rows_grad)) if stream is None and workspace is None else None
+    code = _code(_ACTIVATIONS, activation)
+    if native is not None and code is not None:
+        host, device, raw = native
+        made = host.gated_ff_backward(_address["pipad_gated_ff_backward"], _address["pipad_gated_ff_workspace"], device, raw, X, Wg, Wu, Wd, bg, bu, None,
+                                      code, dY, dX if rows_grad else None, bool(weights), bool(biases))
+        if made is not None:
+            if made[0]:
+                _check(made[0])
+            return GatedFFGrads(dX if rows_grad else None, *made[1:])
     rows = _Rows(X, "X")
     F = rows.width(X)
     x = rows.operand(X, "X")
     block, hidden, Fo = _ff_struct(rows, F, Wg, Wu, Wd, bg, bu, None, activation)
     dy = rows.operand(dY, "dY", Fo)
-    if dX is None and rows_grad:
+    if not rows_grad:
+        dX = None
+    elif dX is None:
         dX = rows.room(F)
     shapes = [(F, hidden), (F, hidden), (hidden, Fo)] if weights else [None] * 3
     shapes += [(hidden,), (hidden,), (Fo,)] if biases else [None] * 3

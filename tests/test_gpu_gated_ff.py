@@ -253,3 +253,39 @@ def test_tensors_that_do_not_fit(pipad):
                  lambda: pipad.gated_ff(X, *W, workspace=torch.zeros(1, device="cuda"))):
         with pytest.raises(pipad.PipadError):
             call()
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("n,k", [(1, 1), (40, 3), (0, 2), (70, 32)])
+def test_same_bits_with_and_without_the_native_half(pipad, monkeypatch, layout, n, k):
+    from paper_2301_00391_amd import binding
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    F, hidden, Fo = 20, 50, 12
+    W, b = weights(gen, F, hidden, Fo, True, 1)
+    ops = [operands(gen, layout, n, k, F)[1] for _ in range(5)]
+    dY = operands(gen, layout, n, k, Fo)[1]
+    v = [torch.randn(F, device="cuda", generator=gen) for _ in range(5)]
+    seen, host = [], binding._host
+    assert host is not None
+    made = []
+
+    class Seen:
+        def __getattr__(self, name):
+            return lambda *args: made.append(getattr(host, name)(*args)) or made[-1]
+
+    for half in (Seen(), None):
+        monkeypatch.setattr(binding, "_host", half)
+        outs = [room(layout, n, k, F)[1] for _ in range(6)]
+        Y = room(layout, n, k, Fo)[1]
+        pipad.gated_ff(ops[0], *W, *b, Y=Y)
+        d = pipad.gated_ff_backward(ops[0], dY, *W, *b[:2], dX=outs[0])
+        some = pipad.gated_ff_backward(ops[0], dY, *W, *b[:2], rows_grad=False, weights=False)
+        pipad.residual_norm(ops[0], ops[1], ops[2], post="rms", pre="layer", scale=v[0], w_post=v[1], b_post=v[2], w_pre=v[3], b_pre=v[4], R_out=outs[1], Z=outs[2])
+        e = pipad.residual_norm_backward(outs[1], ops[3], ops[4], ops[1], ops[2], post="rms", pre="layer", scale=v[0], w_post=v[1], b_post=v[2], w_pre=v[3],
+                                         dR=outs[3], dB=outs[4], dgate=outs[5])
+        less = pipad.residual_norm_backward(outs[1], ops[3], None, ops[1], post="rms", pre="layer", dR=outs[3], dB=outs[4], biases=False)
+        torch.cuda.synchronize()
+        seen.append([stacked(Y), *map(stacked, outs), *d[1:], *some[4:], *e[3:], less.dscale, less.dw_post, less.dw_pre])
+        assert some[:4] == (None,) * 4 and less.db_post is None and less.db_pre is None and less.dgate is None
+    assert all(torch.equal(x, y) for x, y in zip(*seen))
+    assert len(made) == 6 and all(m is not None for m in made)
