@@ -26,12 +26,27 @@ struct NormArgs {
 
 constexpr int kSums = 5;  // dscale, dw_post, db_post, dw_pre, db_pre
 
-// Sum over the LPR lanes of a row, the same bits in all of them.  256: the whole workgroup, through `lds`, whose turns alternate
-// between two halves so that one barrier a sum is enough.
+// Sum over the LPR lanes of a row, the same bits in all of them: lanes add what their neighbours have, quads, eights and sixteens what the mirror
+// image has, by register moves (a row needs four such sums one after the other: through LDS they are 150 cycles and more each).  256: the whole
+// workgroup, through `lds`, whose turns alternate between two halves so that one barrier a sum is enough.
+template <int CTRL>
+__device__ inline float plus_moved(float x) {
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
 template <int LPR>
 __device__ inline float row_sum(float x, float *lds, int &turn) {
-#pragma unroll
-  for (int d = 1; d < (LPR < 64 ? LPR : 64); d <<= 1) x += __shfl_xor(x, d);
+  if (LPR >= 2) x = plus_moved<0xb1>(x);    // quad_perm: lane ^ 1
+  if (LPR >= 4) x = plus_moved<0x4e>(x);    // quad_perm: lane ^ 2
+  if (LPR >= 8) x = plus_moved<0x141>(x);   // row_half_mirror
+  if (LPR >= 16) x = plus_moved<0x140>(x);  // row_mirror
+  if (LPR >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if (LPR >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
   if (LPR == 256) {
     float *const at = lds + 4 * turn;
     turn ^= 1;
@@ -44,6 +59,8 @@ __device__ inline float row_sum(float x, float *lds, int &turn) {
 
 __device__ inline float sigmoid_of(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 // The columns of a lane: VEC consecutive ones, NV times, LPR * VEC apart.
 template <int VEC, int LPR, int NV>
 struct Row {
@@ -54,16 +71,20 @@ struct Row {
 #pragma unroll
     for (int j = 0; j < kElems; ++j) v[j] = x;
   }
+  // (vectors, which all rows read, by ordinary loads; matrices are read, and written, once: past the caches)
+  template <bool ONCE = false>
   __device__ void load(const float *p, int lane, int F) {
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
       const int c = column(lane, q * VEC);
       if (VEC == 4) {
-        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < F) t = *reinterpret_cast<const float4 *>(p + c);
-        v[q * VEC] = t.x, v[q * VEC + 1 % VEC] = t.y, v[q * VEC + 2 % VEC] = t.z, v[q * VEC + 3 % VEC] = t.w;
+        f32x4 t = {0.f, 0.f, 0.f, 0.f};
+        if (c < F) t = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p + c)) : *reinterpret_cast<const f32x4 *>(p + c);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[q * VEC + e] = t[e];
       } else {
-        v[q] = c < F ? p[c] : 0.f;
+        v[q] = 0.f;
+        if (c < F) v[q] = ONCE ? __builtin_nontemporal_load(p + c) : p[c];
       }
     }
   }
@@ -76,8 +97,14 @@ struct Row {
     for (int q = 0; q < NV; ++q) {
       const int c = column(lane, q * VEC);
       if (c < F) {
-        if (VEC == 4) *reinterpret_cast<float4 *>(p + c) = make_float4(v[q * VEC], v[q * VEC + 1 % VEC], v[q * VEC + 2 % VEC], v[q * VEC + 3 % VEC]);
-        else p[c] = v[q];
+        if (VEC == 4) {
+          f32x4 t;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) t[e] = v[q * VEC + e];
+          __builtin_nontemporal_store(t, reinterpret_cast<f32x4 *>(p + c));
+        } else {
+          __builtin_nontemporal_store(v[q], p + c);
+        }
       }
     }
   }
@@ -139,12 +166,14 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm(NormArgs a) {
     w_pre.load_or(a.w_pre, lane, F, 1.f);
     b_pre.load_or(a.b_pre, lane, F, 0.f);
   }
-  for (int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR; i < a.n; i += (int64_t)gridDim.x * kRows) {
+  const int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR;
+  if (i >= a.n) return;  // (with LPR == 256 all of a workgroup's threads, else all lanes of a row)
+  {
     R r, p, gate;
-    r.load(a.R[t] + i * a.ldr, lane, F);
+    r.template load<true>(a.R[t] + i * a.ldr, lane, F);
     if (a.has_b) {
-      p.load(a.B[t] + i * a.ldb, lane, F);
-      if (a.has_gate) gate.load(a.gate[t] + i * a.ldg, lane, F);
+      p.template load<true>(a.B[t] + i * a.ldb, lane, F);
+      if (a.has_gate) gate.template load<true>(a.gate[t] + i * a.ldg, lane, F);
       if (a.post != PIPAD_NORM_NONE) {
         normalise(p, a.post, lane, F, a.inv_f, a.eps, lds, turn);
 #pragma unroll
@@ -173,6 +202,7 @@ template <int VEC, int LPR, int NV>
 __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
   using R = Row<VEC, LPR, NV>;
   constexpr int E = R::kElems, kRows = kBlock / LPR;
+  constexpr bool kAhead = E <= 4;  // a row's loads are on the way while the one before is computed
   __shared__ float lds[8];
   extern __shared__ float sums[];  // [kRows][E * LPR] (more than one row a workgroup)
   int turn = 0;
@@ -184,16 +214,28 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
   w_pre.load_or(a.w_pre, lane, F, 1.f);
 #pragma unroll
   for (int q = 0; q < kSums; ++q) acc[q].fill(0.f);
-  for (int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR; i < a.n; i += (int64_t)gridDim.x * kRows) {
-    R d, b, gate, g;
-    if (a.has_b) b.load(a.B[t] + i * a.ldb, lane, F);
-    if (a.has_gate) gate.load(a.gate[t] + i * a.ldg, lane, F);
-    if (a.has_drout) g.load(a.dRout[t] + i * a.lddro, lane, F);
-    else g.fill(0.f);
+  struct Loaded {
+    R b, gate, g, x, d;
+  };
+  const auto load = [&](Loaded &q, int64_t i) {
+    if (a.has_b) q.b.template load<true>(a.B[t] + i * a.ldb, lane, F);
+    if (a.has_gate) q.gate.template load<true>(a.gate[t] + i * a.ldg, lane, F);
+    if (a.has_drout) q.g.template load<true>(a.dRout[t] + i * a.lddro, lane, F);
+    else q.g.fill(0.f);
     if (a.has_dz) {
-      R x;
-      x.load(a.R[t] + i * a.ldr, lane, F);
-      d.load(a.dZ[t] + i * a.lddz, lane, F);
+      q.x.template load<true>(a.R[t] + i * a.ldr, lane, F);
+      q.d.template load<true>(a.dZ[t] + i * a.lddz, lane, F);
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR;
+  Loaded next;
+  if (kAhead && i < a.n) load(next, i);
+  for (; i < a.n; i += step) {
+    if (!kAhead) load(next, i);
+    R d = next.d, b = next.b, gate = next.gate, g = next.g, x = next.x;
+    if (kAhead && i + step < a.n) load(next, i + step);
+    if (a.has_dz) {
       const float r = normalise(x, a.pre, lane, F, a.inv_f, a.eps, lds, turn);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
@@ -263,27 +305,29 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
 struct SumOut {
   float *out[kSums];
 };
-// out[q][c] = the sum of the workgroups' partial[.][q][c], always in the same order: 16 of its lanes take every 16th each.
-__global__ void __launch_bounds__(kBlock) k_norm_sums(const float *partial, int64_t count, int32_t F, SumOut o) {
-  __shared__ float part[16][17];
+// out[q][c] = the sum of the workgroups' partial[.][q][c], always in the same order: 64 of its lanes take every 64th each.
+constexpr int kSumThreads = 1024, kSumLanes = kSumThreads / 16;
+__global__ void __launch_bounds__(kSumThreads) k_norm_sums(const float *partial, int64_t count, int32_t F, SumOut o) {
+  __shared__ float part[kSumLanes][17];
   const int x = threadIdx.x % 16, y = threadIdx.x / 16;
-  const int64_t c = (int64_t)blockIdx.x * 16 + x;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  if (c < (int64_t)kSums * F) {
+  const int64_t c = (int64_t)blockIdx.x * 16 + x, columns = (int64_t)kSums * F;
+  float s[8] = {};
+  if (c < columns) {
     int64_t b = y;
-    for (; b + 48 < count; b += 64) {
+    for (; b + 7 * kSumLanes < count; b += 8 * kSumLanes) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[u] += partial[(b + 16 * u) * kSums * F + c];
+      for (int u = 0; u < 8; ++u) s[u] += partial[(b + kSumLanes * u) * columns + c];
     }
-    for (; b < count; b += 16) s[0] += partial[b * kSums * F + c];
+    for (; b < count; b += kSumLanes) s[0] += partial[b * columns + c];
   }
-  part[y][x] = (s[0] + s[1]) + (s[2] + s[3]);
-  __syncthreads();
-  if (y != 0 || c >= (int64_t)kSums * F) return;
-  float all = 0.f;
-  for (int w = 0; w < 16; ++w) all += part[w][x];
+  part[y][x] = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+  for (int d = kSumLanes / 2; d >= 1; d /= 2) {
+    __syncthreads();
+    if (y < d) part[y][x] += part[y + d][x];
+  }
+  if (y != 0 || c >= columns) return;
   const int q = (int)(c / F);
-  if (o.out[q]) o.out[q][c - (int64_t)q * F] = all;
+  if (o.out[q]) o.out[q][c - (int64_t)q * F] = part[0][x];
 }
 
 using NormKernel = void (*)(NormArgs);
@@ -297,8 +341,9 @@ NormPlan plan_of() {
   return {k_residual_norm<VEC, LPR, NV>, k_residual_norm_backward<VEC, LPR, NV>, LPR, VEC * NV};
 }
 
-// The fewest lanes that hold a row with one load each, up to a wave; then up to four (16 single) columns a lane more, then the
-// whole workgroup.  `vec`: every row starts on 16 bytes and is a multiple of 4 long.
+// The fewest lanes that hold a row with one load each, up to a wave; then up to four 16-byte pieces (16 single columns) a lane; then the whole
+// workgroup.  `vec`: every row of the call starts on 16 bytes and is a multiple of 4 long.  Others go column by column: 150 thousand rows of 253
+// took 127 us so and 155 in 16-byte pieces off their boundaries, with the loads and stores past the caches or not.
 NormPlan plan(int32_t F, bool vec) {
   if (vec) {
     if (F <= 4) return plan_of<4, 1, 1>();
@@ -326,24 +371,28 @@ NormPlan plan(int32_t F, bool vec) {
   return plan_of<1, 256, 16>();
 }
 
-// Workgroups a snapshot: rows for all of them, at most about 8 a compute unit over all snapshots.
-constexpr int kMostGroups = 2048;
-int64_t groups(int32_t n, int32_t k, int lanes) {
-  const int64_t rows = kBlock / lanes, all = ((int64_t)n + rows - 1) / rows;
-  return std::max<int64_t>(1, std::min<int64_t>(all, (kMostGroups + k - 1) / k));
-}
-
 bool aligned(const float *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 4 == 0; }
+
+// Workgroups a snapshot.  Forward: one for every kBlock / lanes rows, which keeps more loads on the way than fewer that go on and on (8 million rows
+// of 64: 1.67 ms, 2.00 with 2048).  Backward, where each has partial sums: at most 2048 over all snapshots
+// (4 million rows of 128: 3.18 ms with 1024, 3.13 with 2048, 3.22 with 4096).
+constexpr int kMostGroups = 2048;
+int64_t all_groups(int32_t n, int lanes) {
+  const int64_t rows = kBlock / lanes;
+  return ((int64_t)n + rows - 1) / rows;
+}
+int64_t groups(int32_t n, int32_t k, int lanes) { return std::max<int64_t>(1, std::min<int64_t>(all_groups(n, lanes), (kMostGroups + k - 1) / k)); }
 
 }  // namespace
 
 size_t residual_norm_workspace(int32_t F, int32_t n, int32_t k) {
   if (n == 0) return 0;
-  // (the rows' alignment is not known here: the most workgroups that any layout takes)
-  return (size_t)groups(n, k, 256) * k * kSums * F * sizeof(float);
+  // (the rows' alignment is not known here: the more workgroups)
+  return (size_t)std::max(groups(n, k, plan(F, true).lanes), groups(n, k, plan(F, false).lanes)) * k * kSums * F * sizeof(float);
 }
 
-static int fill(NormArgs *a, const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m) {
+// Returns whether every row is one for 16-byte pieces.
+static bool fill(NormArgs *a, const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m) {
   a->n = n, a->F = c.F, a->post = c.post, a->pre = c.pre, a->eps = c.eps, a->inv_f = 1.f / (float)c.F;
   a->scale = c.scale, a->w_post = c.w_post, a->b_post = c.b_post, a->w_pre = c.w_pre, a->b_pre = c.b_pre;
   a->has_b = m.B != nullptr, a->has_gate = m.gate != nullptr, a->has_drout = m.dRout != nullptr, a->has_dz = m.dZ != nullptr;
@@ -365,7 +414,7 @@ static int fill(NormArgs *a, const pipad_residual_norm_t &c, int32_t n, int32_t 
 int residual_norm_launch(const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m, hipStream_t st) {
   NormArgs a{};
   const NormPlan p = plan(c.F, fill(&a, c, n, k, m));
-  hipLaunchKernelGGL(p.forward, dim3((unsigned)groups(n, k, p.lanes), (unsigned)k), dim3(kBlock), 0, st, a);
+  hipLaunchKernelGGL(p.forward, dim3((unsigned)all_groups(n, p.lanes), (unsigned)k), dim3(kBlock), 0, st, a);
   PIPAD_HIP(hipGetLastError());
   return PIPAD_OK;
 }
@@ -390,7 +439,7 @@ int residual_norm_backward_launch(const pipad_residual_norm_t &c, int32_t n, int
     PIPAD_HIP(hipGetLastError());
   }
   if (any) {
-    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((kSums * (int64_t)c.F + 15) / 16)), dim3(kBlock), 0, st,
+    hipLaunchKernelGGL(k_norm_sums, dim3((unsigned)((kSums * (int64_t)c.F + 15) / 16)), dim3(kSumThreads), 0, st,
                        static_cast<const float *>(workspace), count, c.F, o);
     PIPAD_HIP(hipGetLastError());
   }
