@@ -445,15 +445,15 @@ __global__ void __launch_bounds__(kBlock) k_ff_sums(SumArgs a) {
 // ---- host ---------------------------------------------------------------------------------------
 bool aligned(const float *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 4 == 0; }
 
-// Tiles of up to 128 columns: as many as one of the kernels that keep a row has; behind the columns that there are the fragments hold 0.
-constexpr int kKept = 128;
+// Tiles of up to 256 columns: as many as one of the kernels that keep a row has; behind the columns that there are the fragments hold 0.
+constexpr int kKept = 256;
 int32_t column_tiles(int32_t F) {
   const int32_t t = (int32_t)tiles(F, kTile);
-  return F > kKept || t <= 2 ? t : 4;
+  return F > kKept || t <= 2 ? t : t <= 4 ? 4 : 8;
 }
 int32_t depth_tiles(int32_t F, bool backward) {
   const int32_t t = (int32_t)tiles(F, kDepth);
-  return F > kKept || t <= 2 ? t : t <= 4 ? 4 : t <= 6 && !backward ? 6 : 8;
+  return F > kKept || t <= 2 ? t : t <= 4 ? 4 : t <= 6 && !backward ? 6 : t <= 8 ? 8 : 16;
 }
 
 // What lies where in the workspace (bytes), the same for the size query and the calls.
@@ -483,17 +483,17 @@ struct Plan {
     rows = (int64_t)n * k;
     part_floats = 2 * (int64_t)c.F * c.hidden + (int64_t)c.hidden * c.Fo + 2 * (int64_t)c.hidden + c.Fo;
     // Parts of the rows for the weights' gradients, four tiles of rows at least in each.  Rows of any width: about two waves a SIMD.  Up to
-    // 128 columns, where the tiles are of one snapshot each: as many workgroups (64 hidden columns each) as run at a time.
+    // 256 columns, where the tiles are of one snapshot each: as many workgroups (64 hidden columns each) as run at a time.
     kept = c.F <= kKept && c.Fo <= kKept;
     const int64_t row_tiles = kept ? tiles(n, kTile) * k : tiles(rows, kTile);
-    const int64_t at_a_time = std::max(ft, ot) <= 2 ? 512 : 256;
+    const int64_t at_a_time = std::max(ft, ot) <= 2 ? 512 : std::max(ft, ot) <= 4 ? 256 : 128;
     const int64_t most = std::max<int64_t>(1, kept ? at_a_time / tiles(c.hidden, 16 * kWavesPerBlock) : 2048 / ht);
     tiles_per_part = std::max<int64_t>(4, tiles(row_tiles, most));
     parts = tiles(row_tiles, tiles_per_part);
     // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
     // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; in tiles of rows 16.7 to 18.3 throughout (32 through 128: 5.9, 6.5, 11.5 and 9.4 to 10.3).
-    // Rows of more than 128 columns, 256 through 1024: 47.5, 50.3, 96.9 and 381 at 2048; in tiles 493 to 564.
-    few = !backward && rows <= (kept ? 256 : 2048) && c.F <= kFewMostF;
+    // Rows of 256 columns through 1024: 48, 53, 97 and 192 at 1024, in tiles 157; of more columns the tiles are slower by as much again.
+    few = !backward && rows <= (!kept ? 2048 : std::max(c.F, c.Fo) > 128 ? 768 : 256) && c.F <= kFewMostF;
     partial = take(backward ? (size_t)parts * part_floats * sizeof(float) : 0);
     total = at;
   }
@@ -581,7 +581,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
     const FfArgs a = arguments(c, p, n, k, X, ldx, dY, lddy, dX, lddx, ws);
     if (dX && p.kept) {
       const Kept f = kept_backward(c.activation, p.fq, p.oq);
-      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, kTile * f.waves)), dim3(f.waves * kWave), 0, st, a);
+      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, kTile * f.waves), (unsigned)tiles(p.ft, 4)), dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());
     } else if (dX) {
       const int w = width(p.ft);
@@ -591,7 +591,8 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
     }
     if (grads && p.kept) {
       const Kept f = kept_weights(c.activation, p.ft, p.ot);
-      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(c.hidden, 16 * f.waves), (unsigned)p.parts), dim3(f.waves * kWave), 0, st, a);
+      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(c.hidden, 16 * f.waves), (unsigned)p.parts, (unsigned)tiles(std::max(p.ft, p.ot), 4)),
+                         dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());
     } else if (grads) {
       const int most = std::max(p.ft, p.ot), w = std::min(width(most), 1);

@@ -1,4 +1,4 @@
-// The gated feed-forward block, the gradient of X, on rows of up to 128 columns.
+// The gated feed-forward block, the gradient of X, on rows of up to 256 columns.
 #include "pipad_gated_ff.h"
 
 namespace pipad {
@@ -7,11 +7,12 @@ namespace ff {
 namespace {
 
 // As the forward kernel: X's and dY's pieces stay in registers; the phases of a hidden tile are [Wg, Wu, vectors, Wd] and [Wg, Wu] laid out for
-// the way back.
+// the way back.  Of more than 128 columns of X a workgroup makes the gradient of 128, and another G, U and dH once more for the rest.
 template <int ACT, int FQ, int OQ, int WAVES>
 __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_backward(FfArgs a) {
-  constexpr int FT = FQ <= 2 ? 1 : FQ / 2;
+  constexpr int kAll = FQ <= 2 ? 1 : FQ / 2, FT = kAll < 4 ? kAll : 4;
   constexpr int kGu = gu_words(FQ), kUp = OQ * kFragment, kBack = FT * 4 * kFragment;
+  const int f0 = kAll > FT ? blockIdx.y * FT : 0;
   __shared__ u32x4 in[kGu + kUp], back[kBack];
   const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
   const int64_t base = ((int64_t)blockIdx.x * WAVES + threadIdx.x / kWave) * kTile;
@@ -26,7 +27,7 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_
   for (int f = 0; f < FT; ++f) dx[f] = zeros();
   for (int h = 0; h < a.ht; ++h) {
     staged();
-    stage<WAVES, kBack>(a.back + (int64_t)h * kBack, back);
+    stage<WAVES, kBack>(a.back + ((int64_t)h * kAll + f0) * 4 * kFragment, back);
     Sums sg = no_sums(), su = no_sums();
 #pragma unroll
     for (int q = 0; q < FQ; ++q) {
@@ -64,7 +65,7 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
 #pragma unroll
-  for (int f = 0; f < FT; ++f) store_tile(dx[f], out, f * kTile, a.F, a.vec_o, g);
+  for (int f = 0; f < FT; ++f) store_tile(dx[f], out, (f0 + f) * kTile, a.F, a.vec_o, g);
 }
 
 template <int ACT, int FQ>
@@ -73,12 +74,13 @@ Kept kept_backward_of(int oq) {
     case 1: return {k_ff_kept_backward<ACT, FQ, 1, 4>, 4};
     case 2: return {k_ff_kept_backward<ACT, FQ, 2, 4>, 4};
     case 4: return {k_ff_kept_backward<ACT, FQ, 4, 4>, 4};
-    default: return {k_ff_kept_backward<ACT, FQ, 8, 4>, 4};
+    case 8: return {k_ff_kept_backward<ACT, FQ, 8, 4>, 4};
+    default: return {k_ff_kept_backward<ACT, FQ, 16, 4>, 4};
   }
 }
 template <int ACT>
 Kept kept_backward_of(int fq, int oq) {
-  return fq == 1 ? kept_backward_of<ACT, 1>(oq) : fq == 2 ? kept_backward_of<ACT, 2>(oq) : fq == 4 ? kept_backward_of<ACT, 4>(oq) : kept_backward_of<ACT, 8>(oq);
+  return fq == 1 ? kept_backward_of<ACT, 1>(oq) : fq == 2 ? kept_backward_of<ACT, 2>(oq) : fq == 4 ? kept_backward_of<ACT, 4>(oq) : fq == 8 ? kept_backward_of<ACT, 8>(oq) : kept_backward_of<ACT, 16>(oq);
 }
 }  // namespace
 

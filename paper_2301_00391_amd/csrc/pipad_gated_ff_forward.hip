@@ -1,4 +1,4 @@
-// The gated feed-forward block, forward, on rows of up to 128 columns.
+// The gated feed-forward block, forward, on rows of up to 256 columns.
 #include "pipad_gated_ff.h"
 
 namespace pipad {
@@ -10,7 +10,7 @@ namespace {
 // two phases, [Wg, Wu, vectors] and [Wd], each into a buffer of its own while the other is multiplied: loaded past the registers, one
 // barrier a phase.
 template <int ACT, int FQ, int OT, int WAVES>
-__global__ void __launch_bounds__(WAVES *kWave, 2) k_ff_kept(FfArgs a) {
+__global__ void __launch_bounds__(WAVES *kWave, FQ + 2 * OT <= 16 ? 2 : 1) k_ff_kept(FfArgs a) {
   constexpr int kGu = gu_words(FQ), kDown = OT * 2 * kFragment;
   __shared__ u32x4 gu[kGu], down[kDown];  // (two arrays: what is read of one does not wait for what is loaded into the other)
   const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
@@ -53,12 +53,13 @@ __global__ void __launch_bounds__(WAVES *kWave, 2) k_ff_kept(FfArgs a) {
 
 template <int ACT, int FQ, int OT>
 Kept kept_of() {
-  constexpr int kWaves = FQ <= 4 && OT <= 2 ? 4 : 8;
+  // two workgroups a compute unit, or where LDS holds one, twice the waves; above 256 registers a wave it is four again
+  constexpr int kWaves = (FQ <= 4 && OT <= 2) || FQ + 2 * OT > 16 ? 4 : 8;
   return {k_ff_kept<ACT, FQ, OT, kWaves>, kWaves};
 }
 template <int ACT, int FQ>
 Kept kept_of(int ot) {
-  return ot == 1 ? kept_of<ACT, FQ, 1>() : ot == 2 ? kept_of<ACT, FQ, 2>() : kept_of<ACT, FQ, 4>();
+  return ot == 1 ? kept_of<ACT, FQ, 1>() : ot == 2 ? kept_of<ACT, FQ, 2>() : ot == 4 ? kept_of<ACT, FQ, 4>() : kept_of<ACT, FQ, 8>();
 }
 template <int ACT>
 Kept kept_of(int fq, int ot) {
@@ -67,7 +68,8 @@ Kept kept_of(int fq, int ot) {
     case 2: return kept_of<ACT, 2>(ot);
     case 4: return kept_of<ACT, 4>(ot);
     case 6: return kept_of<ACT, 6>(ot);
-    default: return kept_of<ACT, 8>(ot);
+    case 8: return kept_of<ACT, 8>(ot);
+    default: return kept_of<ACT, 16>(ot);
   }
 }
 }  // namespace

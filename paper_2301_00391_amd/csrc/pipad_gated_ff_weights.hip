@@ -1,4 +1,4 @@
-// The gated feed-forward block, the gradients of the weights, on rows of up to 128 columns.
+// The gated feed-forward block, the gradients of the weights, on rows of up to 256 columns.
 //
 // A wave owns 16 hidden columns: it keeps their weights' pieces in registers and accumulates their gradients there.  The four waves of a
 // workgroup share the node rows, 32 of one snapshot at a time, whose pieces lie in LDS row by row in two slots, so that one barrier
@@ -6,6 +6,9 @@
 // dG, dU and H are operands of products whose depth is the node rows; the other operand, X or dY with its columns along the lanes, comes from
 // the same LDS rows by loads that transpose.  It keeps its rows' scales there, by whose inverses dG, dU and H are multiplied before they get a
 // scale of their own: a lane's, since a lane is a hidden column of theirs and of the result.
+//
+// Of more than 128 columns a workgroup accumulates the gradients that go with 128 of X's and 128 of Y's, and another makes G, U and dH once more
+// for the rest: all of them do not fit the registers.
 //
 // Everything is in 16 x 16 x 32 instructions: 16 columns a wave rather than 32 halve the registers for weights and gradients, so that two
 // waves share a SIMD and one's elementwise work runs beside the other's matrix instructions.
@@ -105,11 +108,12 @@ struct Share {
     if (!there()) return;
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
-      uint32_t x = __float_as_uint(largest_of(v[q]));  // of a row: its lanes are 4, 8 or 16 neighbours (not negative: floats compare as integers)
+      uint32_t x = __float_as_uint(largest_of(v[q]));  // of a row: its lanes are 4 to 32 neighbours (not negative: floats compare as integers)
       x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));   // quad_perm: lane ^ 1
       x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));   // quad_perm: lane ^ 2
       if (kChunks >= 8) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));   // row_half_mirror: the other four
       if (kChunks >= 16) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));  // row_mirror: the other eight
+      if (kChunks >= 32) x = __float_as_uint(max_over_16(__uint_as_float(x)));
       const Scale scale = scale_for(__uint_as_float(x));
       slot.put(row(q), chunk(), split8<false>(v[q], sign * scale.to));
       if (chunk() == 0) slot.inv[row(q)] = scale.inv;
@@ -126,6 +130,9 @@ __device__ inline float pieces_of(const float (&v)[8], Split *to) {
 
 template <int ACT, int FD, int OD>
 __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weights(FfArgs a) {
+  constexpr int FS = FD < 4 ? FD : 4, OS = OD < 4 ? OD : 4;  // tiles of 32 columns whose gradients are accumulated here, from f0 and o0 on
+  const int f0 = FD > FS ? blockIdx.z * FS : 0, o0 = OD > OS ? blockIdx.z * OS : 0;
+  const bool mine_f = FD > FS || blockIdx.z == 0, mine_o = OD > OS || blockIdx.z == 0;
   __shared__ Slot<FD> xs[2];
   __shared__ Slot<OD> dys[2];
   const int lane = threadIdx.x & (kWave - 1), l = lane & 15, g = lane >> 4;
@@ -167,11 +174,11 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
     for (int q = 0; q < OD; ++q) wd[q] = split8<false>(v[q], scale.to);
   }
   const float bg = there && a.bg ? a.bg[hid] : 0.f, bu = there && a.bu ? a.bu[hid] : 0.f;
-  f32x4 dwg[2 * FD], dwu[2 * FD], dwd[2 * OD];  // dwd transposed: its rows are Y's columns
+  f32x4 dwg[2 * FS], dwu[2 * FS], dwd[2 * OS];  // dwd transposed: its rows are Y's columns
 #pragma unroll
-  for (int t = 0; t < 2 * FD; ++t) dwg[t] = dwu[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < 2 * FS; ++t) dwg[t] = dwu[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < 2 * OD; ++t) dwd[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < 2 * OS; ++t) dwd[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   Total dbg, dbu, dbd[8];
 
   // the part's tiles, of each snapshot a whole number, and the place of the one that is loaded next
@@ -193,7 +200,7 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   };
   const auto lay_down = [&](int slot, float sign) {
     x.lay_down(xs[slot], sign);
-    if (blockIdx.x == 0)
+    if (blockIdx.x == 0 && blockIdx.z == 0)
 #pragma unroll
       for (int q = 0; q < Share<OD>::kMine; ++q)
 #pragma unroll
@@ -210,18 +217,22 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   for (int64_t i = 0; i < count; ++i) {
     const Slot<FD> &X = xs[i & 1];
     const Slot<OD> &dY = dys[i & 1];
-    f32x4 sg[2], su[2], sd[2];
+    f32x4 sg[2] = {zero, zero}, su[2] = {zero, zero}, sd[2] = {zero, zero};
+    // an operand's loads are on the way while the one before is multiplied (one wave a SIMD waits for each of them otherwise)
+    constexpr int kPlain = 2 * (FD + OD);
+    const auto plain = [&](int p) { return p < 2 * FD ? X.plain(p % 2, p / 2, lane) : dY.plain(p % 2, (p - 2 * FD) / 2, lane); };
+    Split now = plain(0);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      sg[s] = su[s] = sd[s] = zero;
-#pragma unroll
-      for (int q = 0; q < FD; ++q) {
-        const Split p = X.plain(s, q, lane);
-        sg[s] = product16(p, wg[q], sg[s]);
-        su[s] = product16(p, wu[q], su[s]);
+    for (int p = 0; p < kPlain; ++p) {
+      const Split next = plain(p + 1 < kPlain ? p + 1 : 0);
+      if (p < 2 * FD) {
+        sg[p % 2] = product16(now, wg[p / 2], sg[p % 2]);
+        su[p % 2] = product16(now, wu[p / 2], su[p % 2]);
+      } else {
+        sd[p % 2] = product16(now, wd[(p - 2 * FD) / 2], sd[p % 2]);
       }
-#pragma unroll
-      for (int q = 0; q < OD; ++q) sd[s] = product16(dY.plain(s, q, lane), wd[q], sd[s]);
+      now = next;
+      __builtin_amdgcn_sched_barrier(0);
     }
     if (i + 1 < count) {
       lay_down((int)(i + 1) & 1, -sign);
@@ -255,20 +266,36 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
 #pragma unroll
       for (int r = 0; r < 4; ++r) to[r] = fmaf(x[r], factor, to[r]);
     };
+    // likewise, and a product's sums are added while the next one is made
+    constexpr int kTransposed = 2 * (FS + OS);
+    const auto transposed = [&](int p) { return p < 2 * FS ? X.transposed(2 * f0 + p, lane) : dY.transposed(2 * o0 + p - 2 * FS, lane); };
+    f32x4 sums[2];
+    const auto add_sums = [&](int p) {
+      if (p < 2 * FS) {
+        add(dwg[p], cg, sums[0]);
+        add(dwu[p], cu, sums[1]);
+      } else {
+        add(dwd[p - 2 * FS], ch, sums[0]);
+      }
+    };
+    now = transposed(0);
 #pragma unroll
-    for (int q = 0; q < 2 * FD; ++q) {
-      const Split p = X.transposed(q, lane);
-      add(dwg[q], cg, product16(p, dg, zero));
-      add(dwu[q], cu, product16(p, du, zero));
+    for (int p = 0; p < kTransposed; ++p) {
+      const Split next = transposed(p + 1 < kTransposed ? p + 1 : 0);
+      const f32x4 first = product16(now, p < 2 * FS ? dg : hh, zero);
+      const f32x4 second = p < 2 * FS ? product16(now, du, zero) : zero;
+      if (p > 0) add_sums(p - 1);
+      sums[0] = first, sums[1] = second;
+      now = next;
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int q = 0; q < 2 * OD; ++q) add(dwd[q], ch, product16(dY.transposed(q, lane), hh, zero));
+    add_sums(kTransposed - 1);
     __syncthreads();
     sign = -sign;
   }
 
   float *const to = a.partial + blockIdx.y * a.part_floats, *const to_d = to + 2 * (int64_t)a.F * a.hidden, *const to_b = to_d + (int64_t)a.hidden * a.Fo;
-  if (blockIdx.x == 0) {  // dbd: every thread has its columns' sums over its rows
+  if (blockIdx.x == 0 && blockIdx.z == 0) {  // dbd: every thread has its columns' sums over its rows
     float *const sums = reinterpret_cast<float *>(dys);
     constexpr int kThreads = kBlock / Share<OD>::kChunks;  // threads of a chunk of columns
     if (Share<OD>::there())
@@ -289,23 +316,23 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   const float sum_g = over_rows(dbg.sum), sum_u = over_rows(dbu.sum);
   if (there) {
 #pragma unroll
-    for (int q = 0; q < 2 * FD; ++q)
+    for (int q = 0; q < 2 * FS; ++q)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int f = 16 * q + 4 * g + r;
-        if (f < a.F) {
+        const int f = 32 * f0 + 16 * q + 4 * g + r;
+        if (mine_f && f < a.F) {
           to[(int64_t)f * a.hidden + hid] = dwg[q][r];
           to[((int64_t)a.F + f) * a.hidden + hid] = dwu[q][r];
         }
       }
 #pragma unroll
-    for (int q = 0; q < 2 * OD; ++q)
+    for (int q = 0; q < 2 * OS; ++q)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int fo = 16 * q + 4 * g + r;
-        if (fo < a.Fo) to_d[(int64_t)hid * a.Fo + fo] = dwd[q][r];
+        const int fo = 32 * o0 + 16 * q + 4 * g + r;
+        if (mine_o && fo < a.Fo) to_d[(int64_t)hid * a.Fo + fo] = dwd[q][r];
       }
-    if (g == 0) to_b[hid] = sum_g, to_b[a.hidden + hid] = sum_u;
+    if (g == 0 && blockIdx.z == 0) to_b[hid] = sum_g, to_b[a.hidden + hid] = sum_u;
   }
 }
 
@@ -314,12 +341,13 @@ Kept kept_weights_of(int od) {
   switch (od) {
     case 1: return {k_ff_kept_weights<ACT, FD, 1>, kWavesPerBlock};
     case 2: return {k_ff_kept_weights<ACT, FD, 2>, kWavesPerBlock};
-    default: return {k_ff_kept_weights<ACT, FD, 4>, kWavesPerBlock};
+    case 4: return {k_ff_kept_weights<ACT, FD, 4>, kWavesPerBlock};
+    default: return {k_ff_kept_weights<ACT, FD, 8>, kWavesPerBlock};
   }
 }
 template <int ACT>
 Kept kept_weights_of(int fd, int od) {
-  return fd == 1 ? kept_weights_of<ACT, 1>(od) : fd == 2 ? kept_weights_of<ACT, 2>(od) : kept_weights_of<ACT, 4>(od);
+  return fd == 1 ? kept_weights_of<ACT, 1>(od) : fd == 2 ? kept_weights_of<ACT, 2>(od) : fd == 4 ? kept_weights_of<ACT, 4>(od) : kept_weights_of<ACT, 8>(od);
 }
 }  // namespace
 

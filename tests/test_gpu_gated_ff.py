@@ -54,7 +54,7 @@ def check(pipad, n, k, F, hidden, Fo, activation, layout="list", bias=True, pad=
 
 WIDTHS = [(1, 1, 1), (2, 8, 2), (6, 16, 6), (7, 33, 5), (16, 43, 16), (16, 64, 17), (31, 32, 33), (32, 128, 32), (33, 90, 100), (60, 31, 64),
           (64, 171, 64), (64, 256, 64), (65, 100, 128), (100, 77, 31), (128, 341, 100), (128, 65, 128), (129, 40, 3), (3, 40, 129), (200, 130, 256),
-          (256, 70, 200), (300, 33, 20), (17, 1000, 290)]
+          (256, 70, 200), (256, 40, 256), (140, 20, 60), (90, 50, 161), (300, 33, 20), (17, 1000, 290), (257, 40, 300), (320, 70, 257)]
 
 
 @pytest.mark.parametrize("activation", ["sigmoid", "gelu", "silu"])
@@ -65,13 +65,13 @@ def test_every_width(pipad, F, hidden, Fo, activation):
 
 @pytest.mark.parametrize("n,k", [(1, 1), (1, 32), (2, 1), (3, 7), (5, 1), (15, 1), (16, 1), (17, 1), (31, 1), (32, 1), (33, 1), (63, 2), (64, 1), (127, 1), (128, 1),
                                  (129, 3), (511, 1), (700, 32)])
-@pytest.mark.parametrize("F,hidden,Fo", [(16, 43, 16), (64, 100, 60), (150, 64, 40)])
+@pytest.mark.parametrize("F,hidden,Fo", [(16, 43, 16), (64, 100, 60), (150, 64, 40), (270, 64, 20)])
 def test_every_number_of_rows(pipad, n, k, F, hidden, Fo):
     check(pipad, n, k, F, hidden, Fo, "silu")
 
 
 @pytest.mark.parametrize("layout", LAYOUTS)
-@pytest.mark.parametrize("F,hidden,Fo,pad", [(16, 40, 16, 0), (64, 96, 64, 3), (30, 50, 70, 1), (160, 40, 140, 4)])
+@pytest.mark.parametrize("F,hidden,Fo,pad", [(16, 40, 16, 0), (64, 96, 64, 3), (30, 50, 70, 1), (160, 40, 140, 4), (260, 40, 30, 4), (30, 33, 300, 0)])
 def test_every_layout(pipad, layout, F, hidden, Fo, pad):
     check(pipad, 77, 3, F, hidden, Fo, "gelu", layout=layout, pad=pad)
 
@@ -81,7 +81,7 @@ def test_products_keep_the_last_bits_over_a_wide_range_of_magnitudes(pipad, F, h
     check(pipad, 200, 1, F, hidden, Fo, "sigmoid", spread=True)
 
 
-@pytest.mark.parametrize("F,hidden,Fo", [(16, 40, 16), (64, 90, 64), (130, 40, 20)])
+@pytest.mark.parametrize("F,hidden,Fo", [(16, 40, 16), (64, 90, 64), (130, 40, 20), (256, 40, 20), (20, 40, 300)])
 def test_relu_has_no_slope_at_zero(pipad, F, hidden, Fo):
     """Small whole numbers: G is exact, with many zeros, so its sign is no matter of rounding."""
     gen = torch.Generator(device="cuda").manual_seed(F)
@@ -115,7 +115,7 @@ def test_empty_and_partial_results(pipad):
 def test_rows_do_not_see_each_other(pipad):
     """A row that is not finite spoils itself alone, whatever shares its tile."""
     gen = torch.Generator(device="cuda").manual_seed(2)
-    for n, F, hidden, Fo in ((1, 64, 50, 64), (5, 64, 50, 64), (100, 64, 50, 64), (100, 150, 50, 140)):
+    for n, F, hidden, Fo in ((1, 64, 50, 64), (5, 64, 50, 64), (300, 64, 50, 64), (900, 150, 50, 140), (900, 300, 50, 40)):
         W, b = weights(gen, F, hidden, Fo, True)
         X, dY = torch.randn((n, 3, F), device="cuda", generator=gen), torch.randn((n, 3, Fo), device="cuda", generator=gen)
         for bad in (float("inf"), float("nan"), -float("inf")):
@@ -172,7 +172,7 @@ def test_workspace_is_all_that_is_written(pipad):
     from paper_2301_00391_amd import rows
     lib = pipad.load_library()
     gen = torch.Generator(device="cuda").manual_seed(4)
-    for n, k, F, hidden, Fo in ((1, 1, 64, 256, 64), (4, 2, 30, 50, 7), (900, 3, 64, 171, 60), (300, 2, 140, 33, 150)):
+    for n, k, F, hidden, Fo in ((1, 1, 64, 256, 64), (4, 2, 30, 50, 7), (900, 3, 64, 171, 60), (300, 2, 140, 33, 150), (1200, 2, 140, 33, 150), (1200, 2, 260, 33, 150)):
         W, b = weights(gen, F, hidden, Fo, True)
         X, dY = [torch.randn((n, F), device="cuda", generator=gen) for _ in range(k)], [torch.randn((n, Fo), device="cuda", generator=gen) for _ in range(k)]
         block = rows._ff_struct(rows._Rows(X, "X"), F, *W, *b, "silu")[0]
