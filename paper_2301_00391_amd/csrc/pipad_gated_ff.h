@@ -329,7 +329,7 @@ struct Kept {
 };
 Kept kept_forward(int act, int fq, int ot);
 Kept kept_backward(int act, int fq, int oq);
-Kept kept_weights(int act, int fd, int od);  // tiles of 32 columns
+Kept kept_weights(int act, int fd, int od, int waves);  // tiles of 32 columns; 4 waves, or up to 2 tiles 8
 
 }  // namespace ff
 }  // namespace pipad

@@ -463,6 +463,7 @@ struct Plan {
   size_t gu, down, up, back, bd, partial, total;
   int64_t rows, part_floats, parts, tiles_per_part;
   bool kept, few;
+  int weight_waves;
   Plan(const pipad_gated_ff_t &c, int32_t n, int32_t k, bool backward) {
     ht = (int32_t)tiles(c.hidden, kTile);
     fq = depth_tiles(c.F, backward), ft = column_tiles(c.F), oq = depth_tiles(c.Fo, backward), ot = column_tiles(c.Fo);
@@ -486,8 +487,11 @@ struct Plan {
     // 256 columns, where the tiles are of one snapshot each: as many workgroups (64 hidden columns each) as run at a time.
     kept = c.F <= kKept && c.Fo <= kKept;
     const int64_t row_tiles = kept ? tiles(n, kTile) * k : tiles(rows, kTile);
-    const int64_t at_a_time = std::max(ft, ot) <= 2 ? 512 : std::max(ft, ot) <= 4 ? 256 : 128;
-    const int64_t most = std::max<int64_t>(1, kept ? at_a_time / tiles(c.hidden, 16 * kWavesPerBlock) : 2048 / ht);
+    // Eight waves share the rows' splitting where they are all of use (64 columns at most, for the registers): 0.87 of the time of four twice.
+    const int64_t four = tiles(c.hidden, 64), eight = tiles(c.hidden, 128);
+    weight_waves = std::max(ft, ot) <= 2 && 2 * eight * 87 < four * 100 ? 8 : 4;
+    const int64_t at_a_time = weight_waves == 8 ? 256 : std::max(ft, ot) <= 2 ? 512 : std::max(ft, ot) <= 4 ? 256 : 128;
+    const int64_t most = std::max<int64_t>(1, kept ? at_a_time / (weight_waves == 8 ? eight : four) : 2048 / ht);
     tiles_per_part = std::max<int64_t>(4, tiles(row_tiles, most));
     parts = tiles(row_tiles, tiles_per_part);
     // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
@@ -590,7 +594,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
       PIPAD_HIP(hipGetLastError());
     }
     if (grads && p.kept) {
-      const Kept f = kept_weights(c.activation, p.ft, p.ot);
+      const Kept f = kept_weights(c.activation, p.ft, p.ot, p.weight_waves);
       hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(c.hidden, 16 * f.waves), (unsigned)p.parts, (unsigned)tiles(std::max(p.ft, p.ot), 4)),
                          dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());

@@ -78,29 +78,32 @@ struct Slot {
   }
 };
 
-// A thread's share of the rows that come next, 8 columns at a time: 4 D consecutive threads have a row.
-template <int D>
+// A thread's share of the rows that come next, 8 columns at a time: 4 D consecutive threads have a row.  Where there are threads enough X's are the
+// first of a workgroup's THREADS and dY's come behind them, at AT.
+template <int D, int AT, int THREADS>
 struct Share {
-  static constexpr int kMine = kTile * 4 * D / kBlock > 0 ? kTile * 4 * D / kBlock : 1, kChunks = 4 * D;
+  static constexpr int kChunks = 4 * D, kUnits = kTile * kChunks, kMine = kUnits > THREADS ? kUnits / THREADS : 1;
   float v[kMine][8];
-  __device__ static bool there() { return kTile * kChunks >= kBlock || threadIdx.x < kTile * kChunks; }
-  __device__ static int row(int q) { return (q * kBlock + threadIdx.x) / kChunks; }
-  __device__ static int chunk() { return threadIdx.x % kChunks; }
+  __device__ static int me() { return (int)threadIdx.x - AT; }
+  __device__ static bool there() { return AT + kUnits >= THREADS ? AT == 0 || me() >= 0 : me() >= 0 && me() < kUnits; }
+  __device__ static int row(int q) { return (q * THREADS + me()) / kChunks; }
+  __device__ static int chunk() { return me() % kChunks; }
   __device__ void load(const float *first, int64_t ld, int F, bool vec, int count) {  // rows behind `count` are 0
+    if (!there()) return;
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
       const int r = row(q);
       const float *const at = first + (r < count ? r : 0) * ld;
       if (vec && F % 8 == 0) {  // (no column is left out of a piece)
         float4 t[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-        if (there() && r < count && 8 * chunk() < F) {
+        if (r < count && 8 * chunk() < F) {
           t[0] = *reinterpret_cast<const float4 *>(at + 8 * chunk());
           t[1] = *reinterpret_cast<const float4 *>(at + 8 * chunk() + 4);
         }
         v[q][0] = t[0].x, v[q][1] = t[0].y, v[q][2] = t[0].z, v[q][3] = t[0].w;
         v[q][4] = t[1].x, v[q][5] = t[1].y, v[q][6] = t[1].z, v[q][7] = t[1].w;
       } else {
-        load8(v[q], at, 8 * chunk(), there() && r < count ? F : 0, vec);
+        load8(v[q], at, 8 * chunk(), r < count ? F : 0, vec);
       }
     }
   }
@@ -128,15 +131,18 @@ __device__ inline float pieces_of(const float (&v)[8], Split *to) {
   return scale.inv;
 }
 
-template <int ACT, int FD, int OD>
-__global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weights(FfArgs a) {
+template <int ACT, int FD, int OD, int WAVES>
+__global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_weights(FfArgs a) {
+  constexpr int kThreads = WAVES * kWave;
+  using ShareX = Share<FD, 0, kThreads>;
+  using ShareDY = Share<OD, kTile * 4 * (FD + OD) <= kThreads ? kTile * 4 * FD : 0, kThreads>;
   constexpr int FS = FD < 4 ? FD : 4, OS = OD < 4 ? OD : 4;  // tiles of 32 columns whose gradients are accumulated here, from f0 and o0 on
   const int f0 = FD > FS ? blockIdx.z * FS : 0, o0 = OD > OS ? blockIdx.z * OS : 0;
   const bool mine_f = FD > FS || blockIdx.z == 0, mine_o = OD > OS || blockIdx.z == 0;
   __shared__ Slot<FD> xs[2];
   __shared__ Slot<OD> dys[2];
   const int lane = threadIdx.x & (kWave - 1), l = lane & 15, g = lane >> 4;
-  const int hid = (blockIdx.x * kWavesPerBlock + threadIdx.x / kWave) * 16 + l;  // this lane's hidden column; none: weights of 0
+  const int hid = (blockIdx.x * WAVES + threadIdx.x / kWave) * 16 + l;  // this lane's hidden column; none: weights of 0
   const bool there = hid < a.hidden;
 
   Split wg[FD], wu[FD], wd[OD];
@@ -186,8 +192,8 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   const int64_t first = blockIdx.y * a.tiles_per_part, left = every - first, count = left < a.tiles_per_part ? left : a.tiles_per_part;
   int t = (int)(first / of_snapshot);
   int64_t i0 = first % of_snapshot * kTile, loaded = 0;
-  Share<FD> x;
-  Share<OD> dy;
+  ShareX x;
+  ShareDY dy;
   const auto load_next = [&] {
     const int rows = loaded < count ? (int)(a.n - i0 < kTile ? a.n - i0 : kTile) : 0;
     if (rows > 0) {
@@ -200,9 +206,9 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   };
   const auto lay_down = [&](int slot, float sign) {
     x.lay_down(xs[slot], sign);
-    if (blockIdx.x == 0 && blockIdx.z == 0)
+    if (blockIdx.x == 0 && blockIdx.z == 0 && ShareDY::there())
 #pragma unroll
-      for (int q = 0; q < Share<OD>::kMine; ++q)
+      for (int q = 0; q < ShareDY::kMine; ++q)
 #pragma unroll
         for (int j = 0; j < 8; ++j) dbd[j].add(dy.v[q][j]);
     dy.lay_down(dys[slot], sign);
@@ -297,14 +303,14 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   float *const to = a.partial + blockIdx.y * a.part_floats, *const to_d = to + 2 * (int64_t)a.F * a.hidden, *const to_b = to_d + (int64_t)a.hidden * a.Fo;
   if (blockIdx.x == 0 && blockIdx.z == 0) {  // dbd: every thread has its columns' sums over its rows
     float *const sums = reinterpret_cast<float *>(dys);
-    constexpr int kThreads = kBlock / Share<OD>::kChunks;  // threads of a chunk of columns
-    if (Share<OD>::there())
+    constexpr int kSets = (ShareDY::kMine > 1 ? kThreads : ShareDY::kUnits) / ShareDY::kChunks;  // threads that have a chunk of columns
+    if (ShareDY::there())
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sums[(threadIdx.x / Share<OD>::kChunks) * 32 * OD + 8 * Share<OD>::chunk() + j] = dbd[j].sum;
+      for (int j = 0; j < 8; ++j) sums[ShareDY::me() / ShareDY::kChunks * 32 * OD + 8 * ShareDY::chunk() + j] = dbd[j].sum;
     __syncthreads();
-    for (int c = threadIdx.x; c < a.Fo; c += kBlock) {
+    for (int c = threadIdx.x; c < a.Fo; c += kThreads) {
       float s = 0.f;
-      for (int w = 0; w < (kThreads < kTile ? kThreads : kTile); ++w) s += sums[w * 32 * OD + c];
+      for (int w = 0; w < kSets; ++w) s += sums[w * 32 * OD + c];
       to_b[2 * a.hidden + c] = s;
     }
   }
@@ -336,27 +342,39 @@ __global__ void __launch_bounds__(kBlock, FD + OD <= 4 ? 2 : 1) k_ff_kept_weight
   }
 }
 
+template <int ACT, int FD, int OD>
+Kept kept_weights_of(int waves) {
+  if constexpr (FD <= 2 && OD <= 2) {
+    if (waves == 8) return {k_ff_kept_weights<ACT, FD, OD, 8>, 8};
+  }
+  return {k_ff_kept_weights<ACT, FD, OD, 4>, 4};
+}
 template <int ACT, int FD>
-Kept kept_weights_of(int od) {
+Kept kept_weights_of(int od, int waves) {
   switch (od) {
-    case 1: return {k_ff_kept_weights<ACT, FD, 1>, kWavesPerBlock};
-    case 2: return {k_ff_kept_weights<ACT, FD, 2>, kWavesPerBlock};
-    case 4: return {k_ff_kept_weights<ACT, FD, 4>, kWavesPerBlock};
-    default: return {k_ff_kept_weights<ACT, FD, 8>, kWavesPerBlock};
+    case 1: return kept_weights_of<ACT, FD, 1>(waves);
+    case 2: return kept_weights_of<ACT, FD, 2>(waves);
+    case 4: return kept_weights_of<ACT, FD, 4>(waves);
+    default: return kept_weights_of<ACT, FD, 8>(waves);
   }
 }
 template <int ACT>
-Kept kept_weights_of(int fd, int od) {
-  return fd == 1 ? kept_weights_of<ACT, 1>(od) : fd == 2 ? kept_weights_of<ACT, 2>(od) : fd == 4 ? kept_weights_of<ACT, 4>(od) : kept_weights_of<ACT, 8>(od);
+Kept kept_weights_of(int fd, int od, int waves) {
+  switch (fd) {
+    case 1: return kept_weights_of<ACT, 1>(od, waves);
+    case 2: return kept_weights_of<ACT, 2>(od, waves);
+    case 4: return kept_weights_of<ACT, 4>(od, waves);
+    default: return kept_weights_of<ACT, 8>(od, waves);
+  }
 }
 }  // namespace
 
-Kept kept_weights(int act, int fd, int od) {
+Kept kept_weights(int act, int fd, int od, int waves) {
   switch (act) {
-    case PIPAD_ACT_SIGMOID: return kept_weights_of<PIPAD_ACT_SIGMOID>(fd, od);
-    case PIPAD_ACT_RELU: return kept_weights_of<PIPAD_ACT_RELU>(fd, od);
-    case PIPAD_ACT_GELU: return kept_weights_of<PIPAD_ACT_GELU>(fd, od);
-    default: return kept_weights_of<PIPAD_ACT_SILU>(fd, od);
+    case PIPAD_ACT_SIGMOID: return kept_weights_of<PIPAD_ACT_SIGMOID>(fd, od, waves);
+    case PIPAD_ACT_RELU: return kept_weights_of<PIPAD_ACT_RELU>(fd, od, waves);
+    case PIPAD_ACT_GELU: return kept_weights_of<PIPAD_ACT_GELU>(fd, od, waves);
+    default: return kept_weights_of<PIPAD_ACT_SILU>(fd, od, waves);
   }
 }
 
