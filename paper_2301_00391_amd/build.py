@@ -23,7 +23,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpipad.so")
 SOURCES = ["pipad_api.hip", "pipad_build.hip", "pipad_aggregate.hip", "pipad_transpose.hip",
            "pipad_norm.hip", "pipad_gated_ff.hip", "pipad_gated_ff_forward.hip", "pipad_gated_ff_backward.hip",
-           "pipad_gated_ff_weights.hip", "pipad_ceilings.hip"]
+           "pipad_gated_ff_weights.hip", "pipad_gated_ff_split.hip", "pipad_ceilings.hip"]
 
 
 def hipcc() -> str:

@@ -1,5 +1,5 @@
 // The gated feed-forward block: weights as fragments, the kernels for rows of any width, and the host side.  How the products are
-// made stands in pipad_gated_ff.h; rows of few columns have kernels of their own in pipad_gated_ff_forward.hip, _backward.hip and _weights.hip.
+// made stands in pipad_gated_ff.h; rows of few columns have kernels of their own in pipad_gated_ff_forward.hip, _backward.hip, _weights.hip and, for few rows, _split.hip.
 #include "pipad_gated_ff.h"
 
 namespace pipad {
@@ -447,6 +447,8 @@ bool aligned(const float *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p)
 
 // Tiles of up to 256 columns: as many as one of the kernels that keep a row has; behind the columns that there are the fragments hold 0.
 constexpr int kKept = 256;
+constexpr int kUnits = 256;    // compute units
+constexpr int kKeptTiles = 4;  // of the gradient of X that one workgroup has
 int32_t column_tiles(int32_t F) {
   const int32_t t = (int32_t)tiles(F, kTile);
   return F > kKept || t <= 2 ? t : t <= 4 ? 4 : 8;
@@ -462,7 +464,7 @@ struct Plan {
   int64_t n_gu, n_down, n_up, n_back;
   size_t gu, down, up, back, bd, partial, total;
   int64_t rows, part_floats, parts, tiles_per_part;
-  bool kept, few;
+  bool kept, few, split;
   int weight_waves;
   Plan(const pipad_gated_ff_t &c, int32_t n, int32_t k, bool backward) {
     ht = (int32_t)tiles(c.hidden, kTile);
@@ -495,9 +497,16 @@ struct Plan {
     tiles_per_part = std::max<int64_t>(4, tiles(row_tiles, most));
     parts = tiles(row_tiles, tiles_per_part);
     // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
-    // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; in tiles of rows 16.7 to 18.3 throughout (32 through 128: 5.9, 6.5, 11.5 and 9.4 to 10.3).
-    // Rows of 256 columns through 1024: 48, 53, 97 and 192 at 1024, in tiles 157; of more columns the tiles are slower by as much again.
-    few = !backward && rows <= (!kept ? 2048 : std::max(c.F, c.Fo) > 128 ? 768 : 256) && c.F <= kFewMostF;
+    // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; eight waves to 32 rows 13.1 to 14.1 throughout (32 through 128: 5.9, 6.5, 11.5 and 8.8 to
+    // 9.6; 256 through 1024: 48, 53, 97 and 76 to 81).  The kernels for more than 256 columns are slower: 2048 rows there.
+    few = !backward && rows <= (kept ? 256 : 2048) && c.F <= kFewMostF;
+    // Eight waves to 32 rows instead of one, as long as that is one round of workgroups: two a compute unit forward, one for the gradient of X,
+    // of which 256 columns need two for the same rows.  64 through 256, both with the packing of the weights: 13.8 us instead of 18.7 at
+    // 4096 rows, 16.1 instead of 19.7 at 16384, 24.7 instead of 20.7 at 32768; the gradient 19.5 instead of 27.7, 28.7 instead of 28.2 and
+    // 45.3 instead of 30.2.  256 through 1024 at 4096 rows: 78 instead of 160, the gradient 127 instead of 240.  Fewer than four tiles of
+    // hidden columns are too little to share: 16 through 64 took 8.5 instead of 8.1.
+    const int64_t groups = backward ? tiles(rows, kTile) * tiles(ft, kKeptTiles) : tiles(rows, 2 * kTile);
+    split = kept && ht >= 4 && groups <= kUnits;
     partial = take(backward ? (size_t)parts * part_floats * sizeof(float) : 0);
     total = at;
   }
@@ -563,8 +572,8 @@ int gated_ff_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float
   const int rc = pack(c, p, ws, st);
   if (rc != PIPAD_OK) return rc;
   if (p.kept) {
-    const Kept f = kept_forward(c.activation, p.fq, p.ot);
-    hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, kTile * f.waves)), dim3(f.waves * kWave), 0, st, a);
+    const Kept f = p.split ? split_forward(c.activation, p.ot) : kept_forward(c.activation, p.fq, p.ot);
+    hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, p.split ? kTile : kTile * f.waves)), dim3(f.waves * kWave), 0, st, a);
     PIPAD_HIP(hipGetLastError());
     return PIPAD_OK;
   }
@@ -580,12 +589,14 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
   const Plan p(c, n, k, true);
   char *const ws = static_cast<char *>(workspace);
   if (p.rows > 0) {
-    const int rc = pack(c, p, ws, st);
+    // The kernel for the weights' gradients of rows of up to 256 columns reads the weights as they are.
+    const int rc = dX || !p.kept ? pack(c, p, ws, st) : PIPAD_OK;
     if (rc != PIPAD_OK) return rc;
     const FfArgs a = arguments(c, p, n, k, X, ldx, dY, lddy, dX, lddx, ws);
     if (dX && p.kept) {
-      const Kept f = kept_backward(c.activation, p.fq, p.oq);
-      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, kTile * f.waves), (unsigned)tiles(p.ft, 4)), dim3(f.waves * kWave), 0, st, a);
+      const Kept f = p.split ? split_backward(c.activation, p.ft) : kept_backward(c.activation, p.fq, p.oq);
+      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, p.split ? kTile : kTile * f.waves), (unsigned)tiles(p.ft, kKeptTiles)),
+                         dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());
     } else if (dX) {
       const int w = width(p.ft);
@@ -595,7 +606,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
     }
     if (grads && p.kept) {
       const Kept f = kept_weights(c.activation, p.ft, p.ot, p.weight_waves);
-      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(c.hidden, 16 * f.waves), (unsigned)p.parts, (unsigned)tiles(std::max(p.ft, p.ot), 4)),
+      hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(c.hidden, 16 * f.waves), (unsigned)p.parts, (unsigned)tiles(std::max(p.ft, p.ot), kKeptTiles)),
                          dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());
     } else if (grads) {

@@ -70,6 +70,19 @@ def test_every_number_of_rows(pipad, n, k, F, hidden, Fo):
     check(pipad, n, k, F, hidden, Fo, "silu")
 
 
+@pytest.mark.parametrize("activation", ["silu", "gelu", "sigmoid"])
+@pytest.mark.parametrize("F,hidden,Fo", [(1, 97, 1), (16, 129, 40), (40, 250, 20), (33, 97, 100), (100, 160, 97), (70, 300, 250), (200, 128, 130), (256, 257, 256), (150, 97, 5)])
+@pytest.mark.parametrize("n,k,layout", [(257, 1, "list"), (100, 3, "padded"), (33, 32, "list")])
+def test_every_width_of_four_or_more_hidden_tiles(pipad, F, hidden, Fo, activation, n, k, layout):
+    check(pipad, n, k, F, hidden, Fo, activation, layout=layout, bias=activation != "gelu")
+
+
+@pytest.mark.parametrize("rows", [255, 256, 257, 4095, 4096, 4097, 8191, 8192, 8193, 16383, 16384, 16385])
+@pytest.mark.parametrize("F,hidden,Fo", [(16, 96, 16), (16, 97, 16), (40, 97, 150), (150, 97, 40)])
+def test_rows_on_both_sides_of_a_choice(pipad, rows, F, hidden, Fo):
+    check(pipad, rows, 1, F, hidden, Fo, "silu")
+
+
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("F,hidden,Fo,pad", [(16, 40, 16, 0), (64, 96, 64, 3), (30, 50, 70, 1), (160, 40, 140, 4), (260, 40, 30, 4), (30, 33, 300, 0)])
 def test_every_layout(pipad, layout, F, hidden, Fo, pad):
@@ -79,6 +92,12 @@ def test_every_layout(pipad, layout, F, hidden, Fo, pad):
 @pytest.mark.parametrize("F,hidden,Fo", [(20, 50, 20), (64, 128, 64), (128, 60, 90)])
 def test_products_keep_the_last_bits_over_a_wide_range_of_magnitudes(pipad, F, hidden, Fo):
     check(pipad, 200, 1, F, hidden, Fo, "sigmoid", spread=True)
+
+
+@pytest.mark.parametrize("rows", [300, 17000])
+@pytest.mark.parametrize("F,hidden,Fo", [(20, 100, 20), (64, 128, 64), (128, 130, 90), (250, 99, 100)])
+def test_products_keep_the_last_bits_in_every_kernel(pipad, rows, F, hidden, Fo):
+    check(pipad, rows, 1, F, hidden, Fo, "sigmoid", spread=True)
 
 
 @pytest.mark.parametrize("F,hidden,Fo", [(16, 40, 16), (64, 90, 64), (130, 40, 20), (256, 40, 20), (20, 40, 300)])
@@ -115,7 +134,7 @@ def test_empty_and_partial_results(pipad):
 def test_rows_do_not_see_each_other(pipad):
     """A row that is not finite spoils itself alone, whatever shares its tile."""
     gen = torch.Generator(device="cuda").manual_seed(2)
-    for n, F, hidden, Fo in ((1, 64, 50, 64), (5, 64, 50, 64), (300, 64, 50, 64), (900, 150, 50, 140), (900, 300, 50, 40)):
+    for n, F, hidden, Fo in ((1, 64, 50, 64), (5, 64, 50, 64), (300, 64, 50, 64), (300, 64, 150, 64), (900, 150, 150, 140), (900, 150, 50, 140), (900, 300, 50, 40)):
         W, b = weights(gen, F, hidden, Fo, True)
         X, dY = torch.randn((n, 3, F), device="cuda", generator=gen), torch.randn((n, 3, Fo), device="cuda", generator=gen)
         for bad in (float("inf"), float("nan"), -float("inf")):
@@ -172,7 +191,7 @@ def test_workspace_is_all_that_is_written(pipad):
     from paper_2301_00391_amd import rows
     lib = pipad.load_library()
     gen = torch.Generator(device="cuda").manual_seed(4)
-    for n, k, F, hidden, Fo in ((1, 1, 64, 256, 64), (4, 2, 30, 50, 7), (900, 3, 64, 171, 60), (300, 2, 140, 33, 150), (1200, 2, 140, 33, 150), (1200, 2, 260, 33, 150)):
+    for n, k, F, hidden, Fo in ((1, 1, 64, 256, 64), (4, 2, 30, 50, 7), (900, 3, 64, 171, 60), (7000, 3, 64, 171, 60), (300, 2, 140, 33, 150), (1200, 2, 140, 33, 150), (1200, 2, 260, 33, 150)):
         W, b = weights(gen, F, hidden, Fo, True)
         X, dY = [torch.randn((n, F), device="cuda", generator=gen) for _ in range(k)], [torch.randn((n, Fo), device="cuda", generator=gen) for _ in range(k)]
         block = rows._ff_struct(rows._Rows(X, "X"), F, *W, *b, "silu")[0]
