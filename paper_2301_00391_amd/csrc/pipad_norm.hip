@@ -71,7 +71,9 @@ struct Row {
 #pragma unroll
     for (int j = 0; j < kElems; ++j) v[j] = x;
   }
-  // (vectors, which all rows read, by ordinary loads; matrices are read, and written, once: past the caches)
+  // Vectors, which all rows read, by ordinary loads; matrices in 16-byte pieces are read, and written, once: past the caches.  Column by column
+  // the loads of a lane share cache lines with each other and with the next row's: 34 columns at 4.6 TB/s forward and 4.1 backward, past the
+  // caches 3.4 and 2.9.
   template <bool ONCE = false>
   __device__ void load(const float *p, int lane, int F) {
 #pragma unroll
@@ -84,7 +86,7 @@ struct Row {
         for (int e = 0; e < VEC; ++e) v[q * VEC + e] = t[e];
       } else {
         v[q] = 0.f;
-        if (c < F) v[q] = ONCE ? __builtin_nontemporal_load(p + c) : p[c];
+        if (c < F) v[q] = p[c];
       }
     }
   }
@@ -103,7 +105,7 @@ struct Row {
           for (int e = 0; e < VEC; ++e) t[e] = v[q * VEC + e];
           __builtin_nontemporal_store(t, reinterpret_cast<f32x4 *>(p + c));
         } else {
-          __builtin_nontemporal_store(v[q], p + c);
+          p[c] = v[q];
         }
       }
     }
@@ -196,15 +198,15 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm(NormArgs a) {
   }
 }
 
-// The sums over all rows: every lane adds up those of its rows, then the workgroup's lanes of one column are added in a fixed
-// order and go to its own place in `partial`; k_norm_sums adds the workgroups.
+// The sums over all rows: every lane adds up those of its rows, then the lanes of one column are added, within the waves and then over them, in a
+// fixed order, and go to the workgroup's own place in `partial`; k_norm_sums adds the workgroups.
 template <int VEC, int LPR, int NV>
 __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
   using R = Row<VEC, LPR, NV>;
   constexpr int E = R::kElems, kRows = kBlock / LPR;
   constexpr bool kAhead = E <= 4;  // a row's loads are on the way while the one before is computed
   __shared__ float lds[8];
-  extern __shared__ float sums[];  // [kRows][E * LPR] (more than one row a workgroup)
+  __shared__ float sums[2][kWavesPerBlock][LPR < 256 ? E * LPR : 1];  // (more than one row a workgroup; in turns: one barrier a sum)
   int turn = 0;
   const int lane = threadIdx.x % LPR, t = blockIdx.y, F = a.F;
   R scale, w_post, b_post, w_pre, acc[kSums];
@@ -290,15 +292,16 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
         if (acc[q].column(lane, j) < F) to[q * F + acc[q].column(lane, j)] = acc[q].v[j];
       continue;
     }
-    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < E; ++j) sums[(threadIdx.x / LPR) * (E * LPR) + acc[q].column(lane, j)] = acc[q].v[j];
-    __syncthreads();
-    for (int c = threadIdx.x; c < F; c += kBlock) {
-      float s = 0.f;
-      for (int w = 0; w < kRows; ++w) s += sums[w * (E * LPR) + c];
-      to[q * F + c] = s;
+    for (int j = 0; j < E; ++j) {
+      float x = acc[q].v[j];
+#pragma unroll
+      for (int d = LPR; d < kWave; d *= 2) x += __shfl_xor(x, d);
+      if (threadIdx.x % kWave < LPR) sums[q & 1][threadIdx.x / kWave][acc[q].column(lane, j)] = x;
     }
+    __syncthreads();
+    const auto &of = sums[q & 1];
+    for (int c = threadIdx.x; c < F; c += kBlock) to[q * F + c] = (of[0][c] + of[1][c]) + (of[2][c] + of[3][c]);
   }
 }
 
@@ -333,17 +336,19 @@ __global__ void __launch_bounds__(kSumThreads) k_norm_sums(const float *partial,
 using NormKernel = void (*)(NormArgs);
 struct NormPlan {
   NormKernel forward, backward;
-  int lanes, elems;  // of a row: LPR, VEC * NV
+  int lanes;  // of a row: LPR
 };
 
 template <int VEC, int LPR, int NV>
 NormPlan plan_of() {
-  return {k_residual_norm<VEC, LPR, NV>, k_residual_norm_backward<VEC, LPR, NV>, LPR, VEC * NV};
+  return {k_residual_norm<VEC, LPR, NV>, k_residual_norm_backward<VEC, LPR, NV>, LPR};
 }
 
-// The fewest lanes that hold a row with one load each, up to a wave; then up to four 16-byte pieces (16 single columns) a lane; then the whole
-// workgroup.  `vec`: every row of the call starts on 16 bytes and is a multiple of 4 long.  Others go column by column: 150 thousand rows of 253
-// took 127 us so and 155 in 16-byte pieces off their boundaries, with the loads and stores past the caches or not.
+// In 16-byte pieces the fewest lanes that hold a row with one load each, up to a wave; then up to four pieces a lane; then the whole workgroup.
+// `vec`: every row of the call starts on 16 bytes and is a multiple of 4 long.  Others go column by column (150 thousand rows of 253 took
+// 118 us so and 155 in 16-byte pieces off their boundaries), two to four columns a lane: what a row costs is mostly its sums over lanes,
+// so that few lanes idle and several rows share a wave.  256 MB a matrix, with one column a lane up to 64: 3 columns 395 us forward and 569
+// backward, now 292 and 451; 17 columns 583 and 908, now 293 and 549; 34 columns 603 and 948, now 278 and 531.
 NormPlan plan(int32_t F, bool vec) {
   if (vec) {
     if (F <= 4) return plan_of<4, 1, 1>();
@@ -358,13 +363,17 @@ NormPlan plan(int32_t F, bool vec) {
     return plan_of<4, 256, 4>();
   }
   if (F <= 1) return plan_of<1, 1, 1>();
-  if (F <= 2) return plan_of<1, 2, 1>();
-  if (F <= 4) return plan_of<1, 4, 1>();
-  if (F <= 8) return plan_of<1, 8, 1>();
-  if (F <= 16) return plan_of<1, 16, 1>();
-  if (F <= 32) return plan_of<1, 32, 1>();
-  if (F <= 64) return plan_of<1, 64, 1>();
-  if (F <= 128) return plan_of<1, 64, 2>();
+  if (F <= 2) return plan_of<1, 1, 2>();
+  if (F <= 4) return plan_of<1, 2, 2>();
+  if (F <= 8) return plan_of<1, 4, 2>();
+  if (F <= 12) return plan_of<1, 4, 3>();
+  if (F <= 16) return plan_of<1, 8, 2>();
+  if (F <= 24) return plan_of<1, 8, 3>();
+  if (F <= 32) return plan_of<1, 16, 2>();
+  if (F <= 48) return plan_of<1, 16, 3>();
+  if (F <= 64) return plan_of<1, 16, 4>();
+  if (F <= 96) return plan_of<1, 32, 3>();
+  if (F <= 128) return plan_of<1, 32, 4>();
   if (F <= 256) return plan_of<1, 64, 4>();
   if (F <= 512) return plan_of<1, 64, 8>();
   if (F <= 1024) return plan_of<1, 64, 16>();
@@ -434,8 +443,7 @@ int residual_norm_backward_launch(const pipad_residual_norm_t &c, int32_t n, int
     const int64_t g = groups(n, k, p.lanes);
     a.partial = any ? static_cast<float *>(workspace) : nullptr;
     count = g * k;
-    const size_t lds = any && p.lanes < kBlock ? (size_t)kBlock * p.elems * sizeof(float) : 0;
-    hipLaunchKernelGGL(p.backward, dim3((unsigned)g, (unsigned)k), dim3(kBlock), lds, st, a);
+    hipLaunchKernelGGL(p.backward, dim3((unsigned)g, (unsigned)k), dim3(kBlock), 0, st, a);
     PIPAD_HIP(hipGetLastError());
   }
   if (any) {

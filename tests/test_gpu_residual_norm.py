@@ -79,6 +79,12 @@ def test_every_width(pipad, F, layout):  # noqa: F811
     check(pipad, 70, 2, F, "layer", "rms", layout=layout)
 
 
+@pytest.mark.parametrize("F", [1, 2, 3, 4, 5, 8, 10, 12, 13, 16, 20, 24, 25, 30, 32, 40, 48, 49, 60, 64, 80, 96, 97, 110, 128, 190])
+@pytest.mark.parametrize("n,k", [(1, 1), (259, 3), (2100, 1)])
+def test_rows_that_share_a_wave(pipad, F, n, k):  # noqa: F811
+    check(pipad, n, k, F, "rms", "layer", layout="odd")
+
+
 @pytest.mark.parametrize("pre", ["rms", "layer"])
 @pytest.mark.parametrize("F", [3, 64, 200, 1500])
 def test_before_a_first_block(pipad, F, pre):  # noqa: F811
