@@ -485,8 +485,10 @@ struct Plan {
     bd = take(ot * kTile * sizeof(float));
     rows = (int64_t)n * k;
     part_floats = 2 * (int64_t)c.F * c.hidden + (int64_t)c.hidden * c.Fo + 2 * (int64_t)c.hidden + c.Fo;
-    // Parts of the rows for the weights' gradients, four tiles of rows at least in each.  Rows of any width: about two waves a SIMD.  Up to
-    // 256 columns, where the tiles are of one snapshot each: as many workgroups (64 hidden columns each) as run at a time.
+    // Parts of the rows for the weights' gradients.  Rows of any width: about two waves a SIMD, four tiles of rows at least in each.  Up to
+    // 256 columns, where the tiles are of one snapshot each: as many workgroups (64 hidden columns each) as run at a time, and one tile each
+    // of up to 64, two of more, where there are few (64 columns through 256, backward: 37.7 us instead of 45.4 with four at 256 rows, 46.4
+    // instead of 47.8 at 4096, with one 48.9).
     kept = c.F <= kKept && c.Fo <= kKept;
     const int64_t row_tiles = kept ? tiles(n, kTile) * k : tiles(rows, kTile);
     // Eight waves share the rows' splitting where they are all of use (64 columns at most, for the registers): 0.87 of the time of four twice.
@@ -494,7 +496,7 @@ struct Plan {
     weight_waves = std::max(ft, ot) <= 2 && 2 * eight * 87 < four * 100 ? 8 : 4;
     const int64_t at_a_time = weight_waves == 8 ? 256 : std::max(ft, ot) <= 2 ? 512 : std::max(ft, ot) <= 4 ? 256 : 128;
     const int64_t most = std::max<int64_t>(1, kept ? at_a_time / (weight_waves == 8 ? eight : four) : 2048 / ht);
-    tiles_per_part = std::max<int64_t>(4, tiles(row_tiles, most));
+    tiles_per_part = std::max<int64_t>(!kept ? 4 : row_tiles <= 64 ? 1 : 2, tiles(row_tiles, most));
     parts = tiles(row_tiles, tiles_per_part);
     // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
     // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; eight waves to 32 rows 13.1 to 14.1 throughout (32 through 128: 5.9, 6.5, 11.5 and 8.8 to
