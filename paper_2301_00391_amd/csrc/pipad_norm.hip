@@ -17,6 +17,7 @@ struct NormArgs {
   const float *dRout[PIPAD_MAX_K], *dZ[PIPAD_MAX_K];                     // backward
   float *out0[PIPAD_MAX_K], *out1[PIPAD_MAX_K], *out2[PIPAD_MAX_K];      // R', Z; or dR, dB, dgate
   int64_t ldr, ldb, ldg, lddro, lddz, ld0, ld1, ld2;
+  int64_t first;  // row of the launch's first workgroup
   int32_t n, F, post, pre;
   float eps, inv_f;
   const float *scale, *w_post, *b_post, *w_pre, *b_pre;
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm(NormArgs a) {
     w_pre.load_or(a.w_pre, lane, F, 1.f);
     b_pre.load_or(a.b_pre, lane, F, 0.f);
   }
-  const int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / LPR;
+  const int64_t i = a.first + (int64_t)blockIdx.x * kRows + threadIdx.x / LPR;
   if (i >= a.n) return;  // (with LPR == 256 all of a workgroup's threads, else all lanes of a row)
   {
     R r, p, gate;
@@ -423,8 +424,13 @@ static bool fill(NormArgs *a, const pipad_residual_norm_t &c, int32_t n, int32_t
 int residual_norm_launch(const pipad_residual_norm_t &c, int32_t n, int32_t k, const NormRows &m, hipStream_t st) {
   NormArgs a{};
   const NormPlan p = plan(c.F, fill(&a, c, n, k, m));
-  hipLaunchKernelGGL(p.forward, dim3((unsigned)all_groups(n, p.lanes), (unsigned)k), dim3(kBlock), 0, st, a);
-  PIPAD_HIP(hipGetLastError());
+  constexpr int64_t kMostLaunched = (int64_t)1 << 22;  // (a launch has fewer than 2^32 threads along x)
+  const int64_t all = all_groups(n, p.lanes);
+  for (int64_t at = 0; at < all; at += kMostLaunched) {
+    a.first = at * (kBlock / p.lanes);
+    hipLaunchKernelGGL(p.forward, dim3((unsigned)std::min(all - at, kMostLaunched), (unsigned)k), dim3(kBlock), 0, st, a);
+    PIPAD_HIP(hipGetLastError());
+  }
   return PIPAD_OK;
 }
 

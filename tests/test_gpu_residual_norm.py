@@ -212,3 +212,16 @@ def test_rows_past_32_bit_offsets(pipad):  # noqa: F811
     within(d.dR[0][some], *back["dR"], "dR")
     within(d.dB[0][some], *back["dB"], "dB")
     within(d.dw_post, *back["dw_post"], "dw_post")
+
+
+def test_more_rows_than_a_launch_has_threads_for(pipad):  # noqa: F811
+    """A workgroup has 16 rows of 33 columns, and a launch fewer than 2^32 threads along x: 2^24 workgroups are more than one launch."""
+    n, F = (1 << 28) + 77, 33
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    R, Z = torch.zeros((n, F), device="cuda"), torch.full((n, F), 7.0, device="cuda")
+    some = torch.cat([torch.arange(a, a + 40, device="cuda") for a in (0, (1 << 26) - 20, (1 << 27) - 20, (1 << 28) - 20, n - 40)])
+    R[some] = torch.randn((some.numel(), F), device="cuda", generator=gen)
+    pipad.residual_norm([R], pre="layer", eps=EPS, Z=[Z])
+    want = ResidualNorm(None, None, None, "layer", None, None, None, None, None, EPS)
+    within(Z[some], *want.forward(R[some])["Z"], "Z")
+    assert float(Z.sum(1).abs().max()) < 1e-3 and not bool((Z == 7.0).all(1).any())
