@@ -411,10 +411,9 @@ struct SumArgs {
   pipad_gated_ff_grads_t out;
 };
 // The parts added up, always in the same order, each value to its place.
-__global__ void __launch_bounds__(kBlock) k_ff_sums(SumArgs a) {
-  __shared__ float part[4][kWave];
+__device__ inline void sum_parts(const SumArgs &a, int64_t first, float (&part)[4][kWave]) {
   const int x = threadIdx.x & (kWave - 1), y = threadIdx.x / kWave;
-  const int64_t e = (int64_t)blockIdx.x * kWave + x;
+  const int64_t e = first + x;
   float s[4] = {0.f, 0.f, 0.f, 0.f};
   if (e < a.part_floats) {
     int p = y;
@@ -440,6 +439,14 @@ __global__ void __launch_bounds__(kBlock) k_ff_sums(SumArgs a) {
   if ((q -= a.hidden) < a.hidden) return put(a.out.dbu, 0, a.hidden);
   q -= a.hidden;
   put(a.out.dbd, 0, a.Fo);
+}
+constexpr int64_t kMostSums = (int64_t)1 << 22;  // workgroups (a launch has fewer than 2^32 threads along x)
+__global__ void __launch_bounds__(kBlock) k_ff_sums(SumArgs a) {
+  __shared__ float part[4][kWave];
+  for (int64_t first = (int64_t)blockIdx.x * kWave; first < a.part_floats; first += (int64_t)gridDim.x * kWave) {
+    sum_parts(a, first, part);
+    __syncthreads();
+  }
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -620,7 +627,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
   }
   if (grads) {
     const SumArgs s{reinterpret_cast<const float *>(ws + p.partial), p.part_floats, (int32_t)p.parts, c.F, c.hidden, c.Fo, *grads};
-    hipLaunchKernelGGL(k_ff_sums, dim3((unsigned)tiles(p.part_floats, kWave)), dim3(kBlock), 0, st, s);
+    hipLaunchKernelGGL(k_ff_sums, dim3((unsigned)std::min(tiles(p.part_floats, kWave), kMostSums)), dim3(kBlock), 0, st, s);
     PIPAD_HIP(hipGetLastError());
   }
   return PIPAD_OK;

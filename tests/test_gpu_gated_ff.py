@@ -308,3 +308,23 @@ def test_same_bits_with_and_without_the_native_half(pipad, monkeypatch, layout, 
         assert some[:4] == (None,) * 4 and less.db_post is None and less.db_pre is None and less.dgate is None
     assert all(torch.equal(x, y) for x, y in zip(*seen))
     assert len(made) == 6 and all(m is not None for m in made)
+
+
+def test_weights_of_more_values_than_a_launch_has_threads_for(pipad):
+    """One row, so that every gradient is a product of two vectors; 64 values a workgroup of 256 threads: 2^30 of them are 2^32 threads."""
+    F, hidden, Fo = 17000, 22000, 15000
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    W, _ = weights(gen, F, hidden, Fo, False)
+    assert 2 * F * hidden + hidden * Fo > 1 << 30
+    X, dY = torch.randn((1, F), device="cuda", generator=gen), torch.randn((1, Fo), device="cuda", generator=gen)
+    got = pipad.gated_ff_backward([X], [dY], *W, rows_grad=False)
+    G, U = ((X.double() @ w.double())[0] for w in W[:2])
+    dH = (W[2].double() @ dY[0].double())
+    s = torch.sigmoid(G)
+    # Sums of 2^14 products of random signs, a root of it times their size off by 2^-22 each at most (2^-22 for both factors, 2^-24 for the
+    # additions): some 1e-6 of the sums' own size on average, 1e-5 at the worst of 2^14 of them.
+    for name, g, want in (("dWg", got.dWg, torch.outer(X[0].double(), dH * U * s * (1 + G * (1 - s)))), ("dWu", got.dWu, torch.outer(X[0].double(), dH * G * s)),
+                          ("dWd", got.dWd, torch.outer(G * s * U, dY[0].double()))):
+        error = float((g - want).norm() / want.norm())
+        assert error < 1e-5, (name, error)
+        del want

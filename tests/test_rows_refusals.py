@@ -81,7 +81,7 @@ def test_gated_ff_blocks(status, kw):
 @pytest.mark.parametrize("status,kw", [
     (INVALID, {"n": -1}), (INVALID, {"k": 0}), (INVALID, {"k": 33}), (INVALID, {"X": None}), (INVALID, {"Y": None}), (INVALID, {"ldx": 7}),
     (INVALID, {"ldy": 5}), (INVALID, {"X": pointers(2, 0)}), (INVALID, {"ws": None}), (INVALID, {"ws": P + 4}), (SCRATCH, {"nbytes": 100}),
-    (TOO_LARGE, {"ldx": 1 << 39}), (TOO_LARGE, {"ldy": 1 << 41})])
+    (TOO_LARGE, {"ldx": 1 << 39}), (TOO_LARGE, {"ldy": 1 << 41}), (TOO_LARGE, {"n": (1 << 29) + 1})])
 def test_gated_ff_operands(status, kw):
     lib = pipad.load_library()
     at = dict(n=4, k=2, X=pointers(2), ldx=8, Y=pointers(2), ldy=6, ws=P, nbytes=1 << 40)
