@@ -10,6 +10,10 @@
 // Of more than 128 columns a workgroup accumulates the gradients that go with 128 of X's and 128 of Y's, and another makes G, U and dH once more
 // for the rest: all of them do not fit the registers.
 //
+// 1.6 million rows of 64 through 256: 1.25 ms (252 TFLOP/s of its six products), a quarter of it the rows' pieces on their way through LDS, the vector
+// instructions 69 % of the cycles, the matrix instructions 36 %.  312 thousand rows of 128 through 341, where one wave a SIMD waits for itself: 1.25 ms,
+// 39 % and 19 %.
+//
 // Everything is in 16 x 16 x 32 instructions: 16 columns a wave rather than 32 halve the registers for weights and gradients, so that two
 // waves share a SIMD and one's elementwise work runs beside the other's matrix instructions.
 // l = lane % 16, g = lane / 16: an operand's lane holds row (column) l, depth 8 g .. 8 g + 7; register r of the result is row 4 g + r, column l.

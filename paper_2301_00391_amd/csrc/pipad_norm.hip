@@ -6,6 +6,8 @@
 // Everything about a node row is local to the row but the gradients of the vectors that all rows share, so one pass over the
 // matrices does it: a row lies in the registers of LPR lanes, its sums go over these lanes, and nothing is kept from the
 // forward pass but R' itself.  What is read and written once is all that there is to move: 5 matrices forward, 8 backward.
+// Memory bounds it: 8 million rows of 64, forward, 1.62 ms, 6.3 TB/s (a sum of two large arrays reaches 6.1); 4 million of 128, backward, 3.10 ms,
+// 5.3 TB/s from five matrices to three; 150 thousand of 253, column by column, 5.2 TB/s.
 #include "pipad_internal.h"
 
 namespace pipad {

@@ -246,7 +246,8 @@ def gated_ff(X: Features, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, 
              bu: Optional[torch.Tensor] = None, bd: Optional[torch.Tensor] = None, *, activation: str = "silu", Y: Optional[Features] = None,
              workspace: Optional[torch.Tensor] = None, stream=None) -> Features:
     """pipad_gated_ff: Y = (act(X Wg + bg) * (X Wu + bu)) Wd + bd on the rows of all snapshots, whatever lies between staying on the
-    chip.  Wg and Wu are float32 [F, hidden], Wd [hidden, Fo]; ``activation`` is "silu", "gelu" (the exact one), "relu" or "sigmoid"."""
+    chip.  Wg and Wu are float32 [F, hidden], Wd [hidden, Fo]; ``activation`` is "silu", "gelu" (the exact one), "relu" or "sigmoid".
+    Made for rows of up to 256 columns; many wider ones take longer than matrix products one by one."""
     lib = load_library()
     native = _native((Y,)) if stream is None and workspace is None else None
     code = _code(_ACTIVATIONS, activation)
