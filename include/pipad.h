@@ -339,11 +339,11 @@ int pipad_residual_norm_backward(const pipad_residual_norm_t *norm, int32_t n, i
  *   activation  sigmoid, relu, gelu (the exact one, x * Phi(x)) or silu (x * sigmoid(x))
  *   Wg, Wu      row-major float [F][hidden], row strides ldwg, ldwu >= hidden;  Wd  [hidden][Fo], ldwd >= Fo
  *   bg, bu, bd  float [hidden], [hidden], [Fo], NULL: none
- * Widths of 65536 and more, and more than 2^30 rows in all, are PIPAD_ERR_TOO_LARGE.  Products are those of 32-bit floats to about their last
+ * Widths of 65536 and more, and more than 2^30 rows in all (2^28 of more than 256 columns), are PIPAD_ERR_TOO_LARGE.  Products are those of 32-bit floats to about their last
  * bits, from 16-bit pieces with scales (csrc/pipad_gated_ff.h): a row's values, and the weights of 32 hidden columns, are held to 2^-22 of
  * themselves, small ones to 2^-51 of the row's (block's) largest, in the weights' gradients to 2^-40 of it.  A row with a value that is not
  * finite gives NaN where floats may give an infinity, and no other row sees it.
- *  Made for rows of up to 256 columns: wider ones (more than 2048 of them) take several times what single matrix products would. */
+ *  Made for rows of up to 256 columns: for many wider ones the weights' gradients take several times what single matrix products would. */
 #define PIPAD_ACT_SIGMOID 0
 #define PIPAD_ACT_RELU 1
 #define PIPAD_ACT_GELU 2

@@ -276,7 +276,7 @@ static int check_ff_sizes(const pipad_gated_ff_t *c, int32_t n, int32_t k) {
   if (!c || n < 0 || k < 1 || k > PIPAD_MAX_K || c->F < 1 || c->hidden < 1 || c->Fo < 1) return PIPAD_ERR_INVALID_ARG;
   if (c->activation < PIPAD_ACT_SIGMOID || c->activation > PIPAD_ACT_SILU) return PIPAD_ERR_INVALID_ARG;
   const int32_t lim = 1 << 16;
-  const bool many = (int64_t)n * k > (int64_t)1 << 30;  // (rows that a launch's threads can be counted for)
+  const bool many = (int64_t)n * k > (int64_t)1 << (c->F > 256 || c->Fo > 256 ? 28 : 30);  // (rows that a launch's threads can be counted for)
   return many || c->F >= lim || c->hidden >= lim || c->Fo >= lim ? PIPAD_ERR_TOO_LARGE : PIPAD_OK;
 }
 static int check_ff(const pipad_gated_ff_t *c, int32_t n, int32_t k) {

@@ -1,8 +1,9 @@
 // The gated feed-forward block: weights as fragments, the kernels for rows of any width, and the host side.  How the products are
 // made stands in pipad_gated_ff.h; rows of up to 256 columns have kernels of their own in pipad_gated_ff_forward.hip, _backward.hip, _weights.hip
-// and, for few rows, _split.hip.  The kernels here for wider ones hold no row: they read it again for every hidden tile, and what a wave has no
-// registers for is another wave's, which makes G and U again.  65536 rows of 512 through 2048: 10.8 ms forward, 18.2 the gradient of X and 78 those of the
-// weights, where three, five and six matrix products of 32-bit floats take 2.7, 4.5 and 5.4.
+// and, for few rows, _split.hip.  The kernels here for wider ones hold no row, but read it again for every hidden tile, and the waves of a workgroup make
+// a tile of H (dG and dU) each for all of them; of more than 512 columns another workgroup makes them again.  65536 rows of 512 through 2048: 3.0 ms
+// forward and 4.7 the gradient of X, where three and five products of float matrices take 2.7 and 4.5 and write H in between (each wave by itself:
+// 10.8 and 18.2); 29 the gradients of the weights (78), where six take 5.4: a column of X is loaded and split again for every hidden tile.
 #include "pipad_gated_ff.h"
 
 namespace pipad {
@@ -111,43 +112,62 @@ __device__ inline Scale scale_of_row(const float *row, int F, int g, bool vec) {
   return scale_for(max_over_32(largest));
 }
 
-// A wave: 32 node rows, OT tiles of Y's columns from tile blockIdx.y * OT on.  Results lie transposed (a node row is a lane's column).
+// A workgroup: 32 node rows, OT tiles of Y's columns a wave.  The waves make a tile of H each, lay its pieces in LDS (in two places by turns, for one
+// barrier), and all multiply all of these, each into its own columns.  Results lie transposed (a node row is a lane's column).
+template <int PIECES>
+struct Shared {  // what a wave gives the others: operands of 16 deep, and a lane's factor
+  u32x4 piece[2][kWavesPerBlock][PIECES * kFragment];
+  float inv[2][kWavesPerBlock][kWave];
+};
+__device__ inline void lay(u32x4 *to, int index, const Split &s, int lane) {
+  to[index * kFragment + lane] = s.p[0], to[index * kFragment + kWave + lane] = s.p[1];
+}
 template <int ACT, int OT>
 __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
-  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
-  const int64_t base = ((int64_t)blockIdx.x * kWavesPerBlock + threadIdx.x / kWave) * kTile;
-  if (base >= a.rows) return;
+  __shared__ Shared<2> hs;
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t base = (int64_t)blockIdx.x * kTile;
   const RowAt at = row_at(a, base, m);
   const float *const x = a.X[at.t] + at.i * a.ldx;
   const Scale scale_x = scale_of_row(x, a.F, g, a.vec_x);
-  const int o0 = blockIdx.y * OT;
+  const int o0 = (blockIdx.y * kWavesPerBlock + wave) * OT;
   f32x16 y[OT];
 #pragma unroll
   for (int o = 0; o < OT; ++o) y[o] = o0 + o < a.ot ? per_row(a.bd + (o0 + o) * kTile, g) : zeros();
-  for (int h = 0; h < a.ht; ++h) {
-    const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
-    const TileVectors &vectors = vectors_of(gu, a.fq);
-    Sums sg = no_sums(), su = no_sums();
-    for (int q = 0; q < a.fq; ++q) {
-      float v[8];
-      load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
-      const Split b = split8<true>(v, scale_x.to);
-      add_product(sg, fragment(gu, 2 * q), b);
-      add_product(su, fragment(gu, 2 * q + 1), b);
-    }
-    const float inv = scale_x.inv * vectors.inv_gu;
-    f32x16 G = value_of(sg, inv, vectors.bg, g);
-    const f32x16 U = value_of(su, inv, vectors.bu, g);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
-    const Scale scale = scale_for(max_over_32(largest_of(G)));
-    const Split b[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)};
-#pragma unroll
-    for (int o = 0; o < OT; ++o)
-      if (o0 + o < a.ot) {
-        const int64_t w = ((int64_t)h * a.ot + o0 + o) * 2;
-        add(y[o], scale.inv * vectors.inv_down, product(fragment(a.down, w + 1), b[1], product(fragment(a.down, w), b[0], zeros())));
+  for (int h0 = 0, turn = 0; h0 < a.ht; h0 += kWavesPerBlock, turn ^= 1) {
+    if (h0 + wave < a.ht) {
+      const u32x4 *const gu = a.gu + (int64_t)(h0 + wave) * gu_words(a.fq);
+      const TileVectors &vectors = vectors_of(gu, a.fq);
+      Sums sg = no_sums(), su = no_sums();
+      for (int q = 0; q < a.fq; ++q) {
+        float v[8];
+        load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
+        const Split b = split8<true>(v, scale_x.to);
+        add_product(sg, fragment(gu, 2 * q), b);
+        add_product(su, fragment(gu, 2 * q + 1), b);
       }
+      const float inv = scale_x.inv * vectors.inv_gu;
+      f32x16 G = value_of(sg, inv, vectors.bg, g);
+      const f32x16 U = value_of(su, inv, vectors.bu, g);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
+      const Scale scale = scale_for(max_over_32(largest_of(G)));
+#pragma unroll
+      for (int s = 0; s < 2; ++s) lay(hs.piece[turn][wave], s, half<false>(G, s, scale.to), lane);
+      hs.inv[turn][wave][lane] = scale.inv * vectors.inv_down;
+    }
+    __syncthreads();
+    const int count = min(a.ht - h0, kWavesPerBlock);
+    for (int w = 0; w < count; ++w) {
+      const Split b[2] = {fragment(hs.piece[turn][w], 0), fragment(hs.piece[turn][w], 1)};
+      const float inv = hs.inv[turn][w][lane];
+#pragma unroll
+      for (int o = 0; o < OT; ++o)
+        if (o0 + o < a.ot) {
+          const int64_t at_w = ((int64_t)(h0 + w) * a.ot + o0 + o) * 2;
+          add(y[o], inv, product(fragment(a.down, at_w + 1), b[1], product(fragment(a.down, at_w), b[0], zeros())));
+        }
+    }
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
@@ -214,55 +234,72 @@ __global__ void __launch_bounds__(kFewThreads) k_ff_few(FfArgs a) {
 }
 
 // ---- the gradient of X --------------------------------------------------------------------------
+// As k_ff_rows, with dG and dU in the place of H.
 template <int ACT, int FT>
 __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
-  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
-  const int64_t base = ((int64_t)blockIdx.x * kWavesPerBlock + threadIdx.x / kWave) * kTile;
-  if (base >= a.rows) return;
+  __shared__ Shared<4> ds;
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t base = (int64_t)blockIdx.x * kTile;
   const RowAt at = row_at(a, base, m);
   const float *const x = a.X[at.t] + at.i * a.ldx, *const dy = a.dY[at.t] + at.i * a.lddy;
   const Scale scale_x = scale_of_row(x, a.F, g, a.vec_x), scale_dy = scale_of_row(dy, a.Fo, g, a.vec_dy);
-  const int f0 = blockIdx.y * FT;
+  const int f0 = (blockIdx.y * kWavesPerBlock + wave) * FT;
   f32x16 dx[FT];
 #pragma unroll
   for (int f = 0; f < FT; ++f) dx[f] = zeros();
-  for (int h = 0; h < a.ht; ++h) {
-    const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
-    const TileVectors &vectors = vectors_of(gu, a.fq);
-    Sums sg = no_sums(), su = no_sums(), sd = no_sums();
-    float v[8];
-    for (int q = 0; q < a.fq; ++q) {
-      load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
-      const Split b = split8<true>(v, scale_x.to);
-      add_product(sg, fragment(gu, 2 * q), b);
-      add_product(su, fragment(gu, 2 * q + 1), b);
-    }
-    for (int q = 0; q < a.oq; ++q) {
-      load8(v, dy, q * kDepth + 8 * g, a.Fo, a.vec_dy);
-      add_product(sd, fragment(a.up, (int64_t)h * a.oq + q), split8<true>(v, scale_dy.to));
-    }
-    const float inv = scale_x.inv * vectors.inv_gu;
-    f32x16 G = value_of(sg, inv, vectors.bg, g), U = value_of(su, inv, vectors.bu, g);
-    const f32x16 dH = value_of(sd, scale_dy.inv * vectors.inv_up);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float2 c = activate_slope<ACT>(G[r]);
-      G[r] = dH[r] * U[r] * c.y;
-      U[r] = dH[r] * c.x;
-    }
-    const Scale scale = scale_for(max_over_32(largest_of(U, largest_of(G))));
-    const Split dg[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)}, du[2] = {half<false>(U, 0, scale.to), half<false>(U, 1, scale.to)};
-#pragma unroll
-    for (int f = 0; f < FT; ++f)
-      if (f0 + f < a.ft) {
-        f32x16 sum = zeros();
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int64_t w = (((int64_t)h * a.ft + f0 + f) * 2 + s) * 2;
-          sum = product(fragment(a.back, w + 1), du[s], product(fragment(a.back, w), dg[s], sum));
-        }
-        add(dx[f], scale.inv * vectors.inv_back, sum);
+  for (int h0 = 0, turn = 0; h0 < a.ht; h0 += kWavesPerBlock, turn ^= 1) {
+    if (h0 + wave < a.ht) {
+      const int h = h0 + wave;
+      const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
+      const TileVectors &vectors = vectors_of(gu, a.fq);
+      Sums sg = no_sums(), su = no_sums(), sd = no_sums();
+      float v[8];
+      for (int q = 0; q < a.fq; ++q) {
+        load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
+        const Split b = split8<true>(v, scale_x.to);
+        add_product(sg, fragment(gu, 2 * q), b);
+        add_product(su, fragment(gu, 2 * q + 1), b);
       }
+      for (int q = 0; q < a.oq; ++q) {
+        load8(v, dy, q * kDepth + 8 * g, a.Fo, a.vec_dy);
+        add_product(sd, fragment(a.up, (int64_t)h * a.oq + q), split8<true>(v, scale_dy.to));
+      }
+      const float inv = scale_x.inv * vectors.inv_gu;
+      f32x16 G = value_of(sg, inv, vectors.bg, g), U = value_of(su, inv, vectors.bu, g);
+      const f32x16 dH = value_of(sd, scale_dy.inv * vectors.inv_up);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float2 c = activate_slope<ACT>(G[r]);
+        G[r] = dH[r] * U[r] * c.y;
+        U[r] = dH[r] * c.x;
+      }
+      const Scale scale = scale_for(max_over_32(largest_of(U, largest_of(G))));
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        lay(ds.piece[turn][wave], s, half<false>(G, s, scale.to), lane);
+        lay(ds.piece[turn][wave], 2 + s, half<false>(U, s, scale.to), lane);
+      }
+      ds.inv[turn][wave][lane] = scale.inv * vectors.inv_back;
+    }
+    __syncthreads();
+    const int count = min(a.ht - h0, kWavesPerBlock);
+    for (int w = 0; w < count; ++w) {
+      Split dg[2], du[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) dg[s] = fragment(ds.piece[turn][w], s), du[s] = fragment(ds.piece[turn][w], 2 + s);
+      const float inv = ds.inv[turn][w][lane];
+#pragma unroll
+      for (int f = 0; f < FT; ++f)
+        if (f0 + f < a.ft) {
+          f32x16 sum = zeros();
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const int64_t at_w = (((int64_t)(h0 + w) * a.ft + f0 + f) * 2 + s) * 2;
+            sum = product(fragment(a.back, at_w + 1), du[s], product(fragment(a.back, at_w), dg[s], sum));
+          }
+          add(dx[f], inv, sum);
+        }
+    }
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
@@ -271,15 +308,15 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
 }
 
 // ---- the gradients of the weights ---------------------------------------------------------------
-// A wave: one tile of hidden columns, the rows of one part, T tiles of X's and of Y's columns from tile blockIdx.z * T on.  Results
-// lie as they are (a hidden column is a lane's column), so dG, dU and H are operands of products whose depth is the node rows; X and dY keep their
+// A workgroup: one tile of hidden columns, the rows of one part, T tiles of X's and of Y's columns a wave.  The waves make dG, dU and H of 32 rows each,
+// lay their pieces in LDS, and all multiply all of these, each with its own columns of X and dY.  Results lie as they are (a hidden column is a lane's column), so dG, dU and H are operands of products whose depth is the node rows; X and dY keep their
 // rows' scales there, by whose inverses dG, dU and H are multiplied before they get a scale of their own, a hidden column each.
 template <int ACT, int T>
 __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
-  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5;
-  const int h = blockIdx.x * kWavesPerBlock + threadIdx.x / kWave;
-  if (h >= a.ht) return;
-  const int t0 = blockIdx.z * T;
+  __shared__ Shared<6> shared;
+  __shared__ float inv_of[2][kWavesPerBlock][2][kWave], to_of[2][kWavesPerBlock][2][kTile], bias[2][kWavesPerBlock][kTile];
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int h = blockIdx.x, t0 = (blockIdx.z * kWavesPerBlock + wave) * T;
   f32x16 dwg[T], dwu[T], dwd[T];  // dwd transposed: its rows are Y's columns
 #pragma unroll
   for (int t = 0; t < T; ++t) dwg[t] = dwu[t] = dwd[t] = zeros();
@@ -289,94 +326,107 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
   const float bg = vectors.bg[m], bu = vectors.bu[m];
   const int64_t first = blockIdx.y * a.tiles_per_part * kTile;
   const int64_t end = first + a.tiles_per_part * kTile < a.rows ? first + a.tiles_per_part * kTile : a.rows;
-  for (int64_t base = first; base < end; base += kTile) {
-    const bool there = base + m < end;
-    const RowAt at = row_at(a, base, m);
-    const float *const x = a.X[at.t] + at.i * a.ldx, *const dy = a.dY[at.t] + at.i * a.lddy;
-    const float sign = base / kTile % 2 ? -1.f : 1.f;
-    const Scale scale_x = scale_of_row(x, there ? a.F : 0, g, a.vec_x), scale_dy = scale_of_row(dy, there ? a.Fo : 0, g, a.vec_dy);
-    Sums sg = no_sums(), su = no_sums(), sd = no_sums();
-    float v[8];
-    for (int q = 0; q < a.fq; ++q) {
-      load8(v, x, q * kDepth + 8 * g, there ? a.F : 0, a.vec_x);
-      const Split b = split8<true>(v, sign * scale_x.to);
-      add_product(sg, b, fragment(gu, 2 * q));
-      add_product(su, b, fragment(gu, 2 * q + 1));
-    }
-    for (int q = 0; q < a.oq; ++q) {
-      load8(v, dy, q * kDepth + 8 * g, there ? a.Fo : 0, a.vec_dy);
-      add_product(sd, split8<true>(v, sign * scale_dy.to), fragment(a.up, (int64_t)h * a.oq + q));
-    }
-    float vg[16], vu[16], vh[16], to_x[16], to_dy[16], tile_g = 0.f, tile_u = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int d = result_depth(r / 8, g, r % 8);
-      const float inv_x = __shfl(scale_x.inv, d), inv_dy = __shfl(scale_dy.inv, d);
-      to_x[r] = __shfl(scale_x.to, d), to_dy[r] = __shfl(scale_dy.to, d);
-      const float cx = sign * vectors.inv_gu * inv_x, cd = sign * vectors.inv_up * inv_dy;
-      const float2 c = activate_slope<ACT>(fmaf(sg.main[r], cx, fmaf(sg.cross[r], cx * (1.f / kWide), bg)));
-      const float u = fmaf(su.main[r], cx, fmaf(su.cross[r], cx * (1.f / kWide), bu)), e = fmaf(sd.main[r], cd, sd.cross[r] * (cd * (1.f / kWide)));
-      vg[r] = e * u * c.y;
-      vu[r] = e * c.x;
-      tile_g += vg[r];
-      tile_u += vu[r];
-      vg[r] *= inv_x;
-      vu[r] *= inv_x;
-      vh[r] = c.x * u * inv_dy;
-    }
-    dbg.add(tile_g), dbu.add(tile_u);
-    const auto pieces = [&](const float (&from)[16], Split (&to)[2]) {
-      const Scale scale = scale_for(max_over_32(largest_of(from)));
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = from[8 * s + j];
-        to[s] = split8<true>(v, scale.to);
+  const auto sign_of = [](int64_t base) { return base / kTile % 2 ? -1.f : 1.f; };
+  int turn = 0;
+  for (int64_t batch = first; batch < end; batch += kWavesPerBlock * kTile, turn ^= 1) {
+    const int64_t mine = batch + wave * kTile;
+    if (mine < end) {
+      const bool there = mine + m < end;
+      const RowAt at = row_at(a, mine, m);
+      const float *const x = a.X[at.t] + at.i * a.ldx, *const dy = a.dY[at.t] + at.i * a.lddy;
+      const float sign = sign_of(mine);
+      const Scale scale_x = scale_of_row(x, there ? a.F : 0, g, a.vec_x), scale_dy = scale_of_row(dy, there ? a.Fo : 0, g, a.vec_dy);
+      Sums sg = no_sums(), su = no_sums(), sd = no_sums();
+      float v[8];
+      for (int q = 0; q < a.fq; ++q) {
+        load8(v, x, q * kDepth + 8 * g, there ? a.F : 0, a.vec_x);
+        const Split b = split8<true>(v, sign * scale_x.to);
+        add_product(sg, b, fragment(gu, 2 * q));
+        add_product(su, b, fragment(gu, 2 * q + 1));
       }
-      return sign * scale.inv;
-    };
-    Split dg[2], du[2], hh[2];
-    const float cg = pieces(vg, dg), cu = pieces(vu, du), ch = pieces(vh, hh);
+      for (int q = 0; q < a.oq; ++q) {
+        load8(v, dy, q * kDepth + 8 * g, there ? a.Fo : 0, a.vec_dy);
+        add_product(sd, split8<true>(v, sign * scale_dy.to), fragment(a.up, (int64_t)h * a.oq + q));
+      }
+      float vg[16], vu[16], vh[16], tile_g = 0.f, tile_u = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int d = result_depth(r / 8, g, r % 8);
+        const float inv_x = __shfl(scale_x.inv, d), inv_dy = __shfl(scale_dy.inv, d);
+        const float cx = sign * vectors.inv_gu * inv_x, cd = sign * vectors.inv_up * inv_dy;
+        const float2 c = activate_slope<ACT>(fmaf(sg.main[r], cx, fmaf(sg.cross[r], cx * (1.f / kWide), bg)));
+        const float u = fmaf(su.main[r], cx, fmaf(su.cross[r], cx * (1.f / kWide), bu)), e = fmaf(sd.main[r], cd, sd.cross[r] * (cd * (1.f / kWide)));
+        vg[r] = e * u * c.y;
+        vu[r] = e * c.x;
+        tile_g += vg[r];
+        tile_u += vu[r];
+        vg[r] *= inv_x;
+        vu[r] *= inv_x;
+        vh[r] = c.x * u * inv_dy;
+      }
+      dbg.add(tile_g), dbu.add(tile_u);
+      const auto pieces = [&](const float (&from)[16], int index) {
+        const Scale scale = scale_for(max_over_32(largest_of(from)));
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = from[8 * s + j];
+          lay(shared.piece[turn][wave], index + s, split8<true>(v, scale.to), lane);
+        }
+        return sign * scale.inv;
+      };
+      shared.inv[turn][wave][lane] = pieces(vg, 0);
+      inv_of[turn][wave][0][lane] = pieces(vu, 2);
+      inv_of[turn][wave][1][lane] = pieces(vh, 4);
+      if (g == 0) to_of[turn][wave][0][m] = sign * scale_x.to, to_of[turn][wave][1][m] = sign * scale_dy.to;
+    }
+    __syncthreads();
     const auto add_sums = [&](f32x16 &to, float factor, const Sums &c) {
       add(to, factor * (1.f / kWide), c.cross);
       add(to, factor, c.main);
     };
+    for (int w = 0; w < kWavesPerBlock && batch + w * kTile < end; ++w) {
+      const int64_t base = batch + w * kTile;
+      const u32x4 *const of = shared.piece[turn][w];
+      const float cg = shared.inv[turn][w][lane], cu = inv_of[turn][w][0][lane], ch = inv_of[turn][w][1][lane];
+      float v[8];
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const int c = (t0 + t) * kTile + m;
-      const auto transposed = [&](const float *const *X, int64_t ld, int F, const float (&to)[16], int s) {
+      for (int t = 0; t < T; ++t) {
+        const int c = (t0 + t) * kTile + m;
+        const auto transposed = [&](const float *const *X, int64_t ld, int F, const float (&to)[kTile], int s) {
+          float scaled[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int d = result_depth(s, g, j);
-          const RowAt r = row_at(a, base, d);
-          v[j] = base + d < end && c < F ? X[r.t][r.i * ld + c] : 0.f;
+          for (int j = 0; j < 8; ++j) {
+            const int d = result_depth(s, g, j);
+            const RowAt r = row_at(a, base, d);
+            v[j] = base + d < end && c < F ? X[r.t][r.i * ld + c] : 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) scaled[j] = v[j] * to[result_depth(s, g, j)];
+          return split8<true>(scaled, 1.f);
+        };
+        if (t0 + t < a.ft) {
+          Sums g_sum = no_sums(), u_sum = no_sums();
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const Split xs = transposed(a.X, a.ldx, a.F, to_of[turn][w][0], s);
+            add_product(g_sum, xs, fragment(of, s));
+            add_product(u_sum, xs, fragment(of, 2 + s));
+          }
+          add_sums(dwg[t], cg, g_sum);
+          add_sums(dwu[t], cu, u_sum);
         }
-        float w[8];
+        if (t0 + t < a.ot) {
+          Sums d_sum = no_sums();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = v[j] * to[8 * s + j];
-        return split8<true>(w, sign);
-      };
-      if (t0 + t < a.ft) {
-        Sums g_sum = no_sums(), u_sum = no_sums();
+          for (int s = 0; s < 2; ++s) {
+            const Split dys = transposed(a.dY, a.lddy, a.Fo, to_of[turn][w][1], s);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const Split xs = transposed(a.X, a.ldx, a.F, to_x, s);
-          add_product(g_sum, xs, dg[s]);
-          add_product(u_sum, xs, du[s]);
+            for (int j = 0; j < 8; ++j) dbd[t].add(v[j]);
+            add_product(d_sum, dys, fragment(of, 4 + s));
+          }
+          add_sums(dwd[t], ch, d_sum);
         }
-        add_sums(dwg[t], cg, g_sum);
-        add_sums(dwu[t], cu, u_sum);
-      }
-      if (t0 + t < a.ot) {
-        Sums d_sum = no_sums();
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const Split ds = transposed(a.dY, a.lddy, a.Fo, to_dy, s);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) dbd[t].add(v[j]);
-          add_product(d_sum, ds, hh[s]);
-        }
-        add_sums(dwd[t], ch, d_sum);
       }
     }
   }
@@ -395,9 +445,11 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
     }
   float *const to_b = to_d + (int64_t)a.hidden * a.Fo;
   const float sum_g = dbg.sum + __shfl_xor(dbg.sum, 32), sum_u = dbu.sum + __shfl_xor(dbu.sum, 32);
-  if (blockIdx.z == 0 && g == 0 && hid < a.hidden) {
-    to_b[hid] = sum_g;
-    to_b[a.hidden + hid] = sum_u;
+  if (g == 0) bias[0][wave][m] = sum_g, bias[1][wave][m] = sum_u;
+  __syncthreads();
+  if (blockIdx.z == 0 && wave == 0 && g == 0 && hid < a.hidden) {
+    to_b[hid] = (bias[0][0][m] + bias[0][1][m]) + (bias[0][2][m] + bias[0][3][m]);
+    to_b[a.hidden + hid] = (bias[1][0][m] + bias[1][1][m]) + (bias[1][2][m] + bias[1][3][m]);
   }
 #pragma unroll
   for (int t = 0; t < T; ++t) {
@@ -495,7 +547,7 @@ struct Plan {
     bd = take(ot * kTile * sizeof(float));
     rows = (int64_t)n * k;
     part_floats = 2 * (int64_t)c.F * c.hidden + (int64_t)c.hidden * c.Fo + 2 * (int64_t)c.hidden + c.Fo;
-    // Parts of the rows for the weights' gradients.  Rows of any width: about two waves a SIMD, four tiles of rows at least in each.  Up to
+    // Parts of the rows for the weights' gradients.  Rows of any width: a thousand workgroups, a tile of rows a wave at least.  Up to
     // 256 columns, where the tiles are of one snapshot each: as many workgroups (64 hidden columns each) as run at a time, and one tile each
     // of up to 64, two of more, where there are few (64 columns through 256, backward: 37.7 us instead of 45.4 with four at 256 rows, 46.4
     // instead of 47.8 at 4096, with one 48.9).
@@ -505,7 +557,7 @@ struct Plan {
     const int64_t four = tiles(c.hidden, 64), eight = tiles(c.hidden, 128);
     weight_waves = std::max(ft, ot) <= 2 && 2 * eight * 87 < four * 100 ? 8 : 4;
     const int64_t at_a_time = weight_waves == 8 ? 256 : std::max(ft, ot) <= 2 ? 512 : std::max(ft, ot) <= 4 ? 256 : 128;
-    const int64_t most = std::max<int64_t>(1, kept ? at_a_time / (weight_waves == 8 ? eight : four) : 2048 / ht);
+    const int64_t most = std::max<int64_t>(1, kept ? at_a_time / (weight_waves == 8 ? eight : four) : 1024 / ht);
     tiles_per_part = std::max<int64_t>(!kept ? 4 : row_tiles <= 64 ? 1 : 2, tiles(row_tiles, most));
     parts = tiles(row_tiles, tiles_per_part);
     // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
@@ -565,7 +617,8 @@ PIPAD_FF_KERNELS(k_ff_rows_backward, 4)
 PIPAD_FF_KERNELS(k_ff_weights_backward, 2)
 #undef PIPAD_FF_KERNELS
 
-int width(int t) { return t <= 1 ? 0 : t <= 2 ? 1 : 2; }  // which of 1, 2, 4 tiles
+// Which of 1, 2, 4 tiles a wave, of the four that share t
+int width(int t) { return t <= kWavesPerBlock ? 0 : t <= 2 * kWavesPerBlock ? 1 : 2; }
 
 }  // namespace
 
@@ -590,7 +643,7 @@ int gated_ff_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float
     return PIPAD_OK;
   }
   const int w = width(p.ot);
-  hipLaunchKernelGGL(k_ff_rows_of[c.activation][w], dim3((unsigned)tiles(p.rows, kTile * kWavesPerBlock), (unsigned)tiles(p.ot, 1 << w)),
+  hipLaunchKernelGGL(k_ff_rows_of[c.activation][w], dim3((unsigned)tiles(p.rows, kTile), (unsigned)tiles(p.ot, kWavesPerBlock << w)),
                      dim3(kBlock), 0, st, a);
   PIPAD_HIP(hipGetLastError());
   return PIPAD_OK;
@@ -613,7 +666,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
     } else if (dX) {
       const int w = width(p.ft);
       hipLaunchKernelGGL(k_ff_rows_backward_of[c.activation][w],
-                         dim3((unsigned)tiles(p.rows, kTile * kWavesPerBlock), (unsigned)tiles(p.ft, 1 << w)), dim3(kBlock), 0, st, a);
+                         dim3((unsigned)tiles(p.rows, kTile), (unsigned)tiles(p.ft, kWavesPerBlock << w)), dim3(kBlock), 0, st, a);
       PIPAD_HIP(hipGetLastError());
     }
     if (grads && p.kept) {
@@ -624,7 +677,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
     } else if (grads) {
       const int most = std::max(p.ft, p.ot), w = std::min(width(most), 1);
       hipLaunchKernelGGL(k_ff_weights_backward_of[c.activation][w],
-                         dim3((unsigned)tiles(p.ht, kWavesPerBlock), (unsigned)p.parts, (unsigned)tiles(most, 1 << w)), dim3(kBlock), 0, st, a);
+                         dim3((unsigned)p.ht, (unsigned)p.parts, (unsigned)tiles(most, kWavesPerBlock << w)), dim3(kBlock), 0, st, a);
       PIPAD_HIP(hipGetLastError());
     }
   }

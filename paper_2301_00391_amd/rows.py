@@ -246,8 +246,7 @@ def gated_ff(X: Features, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, 
              bu: Optional[torch.Tensor] = None, bd: Optional[torch.Tensor] = None, *, activation: str = "silu", Y: Optional[Features] = None,
              workspace: Optional[torch.Tensor] = None, stream=None) -> Features:
     """pipad_gated_ff: Y = (act(X Wg + bg) * (X Wu + bu)) Wd + bd on the rows of all snapshots, whatever lies between staying on the
-    chip.  Wg and Wu are float32 [F, hidden], Wd [hidden, Fo]; ``activation`` is "silu", "gelu" (the exact one), "relu" or "sigmoid".
-    Made for rows of up to 256 columns; many wider ones take longer than matrix products one by one."""
+    chip.  Wg and Wu are float32 [F, hidden], Wd [hidden, Fo]; ``activation`` is "silu", "gelu" (the exact one), "relu" or "sigmoid"."""
     lib = load_library()
     native = _native((Y,)) if stream is None and workspace is None else None
     code = _code(_ACTIVATIONS, activation)
@@ -277,7 +276,8 @@ def gated_ff_backward(X: Features, dY: Features, Wg: torch.Tensor, Wu: torch.Ten
                       biases: bool = True, dX: Optional[Features] = None, workspace: Optional[torch.Tensor] = None,
                       stream=None) -> GatedFFGrads:
     """pipad_gated_ff_backward: from X and dY the gradient of X (unless ``rows_grad=False``), of the matrices (unless ``weights=False``) and
-    of the biases (unless ``biases=False``); G, U and H are made again, so nothing has to be kept from the forward call."""
+    of the biases (unless ``biases=False``); G, U and H are made again, so nothing has to be kept from the forward call.
+    Made for rows of up to 256 columns: for many wider ones the matrices' gradients take longer than products one by one."""
     lib = load_library()
     native = _native((dX,) * bool(rows_grad)) if stream is None and workspace is None else None
     code = _code(_ACTIVATIONS, activation)

@@ -77,6 +77,12 @@ def test_every_width_of_four_or_more_hidden_tiles(pipad, F, hidden, Fo, activati
     check(pipad, n, k, F, hidden, Fo, activation, layout=layout, bias=activation != "gelu")
 
 
+@pytest.mark.parametrize("F,hidden,Fo", [(257, 33, 20), (290, 160, 300), (530, 130, 40), (40, 130, 530), (700, 97, 260), (1100, 40, 3), (600, 257, 1060)])
+@pytest.mark.parametrize("n,k", [(2100, 1), (70, 31)])
+def test_rows_of_more_than_256_columns(pipad, F, hidden, Fo, n, k):
+    check(pipad, n, k, F, hidden, Fo, "silu", layout="padded" if F % 4 else "list")
+
+
 @pytest.mark.parametrize("rows", [255, 256, 257, 4095, 4096, 4097, 8191, 8192, 8193, 16383, 16384, 16385])
 @pytest.mark.parametrize("F,hidden,Fo", [(16, 96, 16), (16, 97, 16), (40, 97, 150), (150, 97, 40)])
 def test_rows_on_both_sides_of_a_choice(pipad, rows, F, hidden, Fo):

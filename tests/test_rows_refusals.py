@@ -91,6 +91,14 @@ def test_gated_ff_operands(status, kw):
     assert lib.pipad_gated_ff_backward(block(), *(at[q] for q in ("n", "k", "X", "ldx", "Y", "ldy")), *dx, None, at["ws"], at["nbytes"], None) == status
 
 
+def test_gated_ff_of_many_wide_rows():
+    lib, got = pipad.load_library(), ctypes.c_size_t()
+    for sizes, most in (({}, 1 << 30), ({"F": 257}, 1 << 28), ({"Fo": 257, "ldwd": 257}, 1 << 28)):
+        for backward in (0, 1):
+            assert lib.pipad_gated_ff_workspace(block(**sizes), most // 32, 32, backward, ctypes.byref(got)) == 0
+            assert lib.pipad_gated_ff_workspace(block(**sizes), most // 32 + 1, 32, backward, ctypes.byref(got)) == TOO_LARGE
+
+
 def test_gated_ff_gradients():
     lib = pipad.load_library()
     x, y = [pointers(2), 8], [pointers(2), 6]
