@@ -309,8 +309,9 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
 
 // ---- the gradients of the weights ---------------------------------------------------------------
 // A workgroup: one tile of hidden columns, the rows of one part, T tiles of X's and of Y's columns a wave.  The waves make dG, dU and H of 32 rows each,
-// lay their pieces in LDS, and all multiply all of these, each with its own columns of X and dY.  Results lie as they are (a hidden column is a lane's column), so dG, dU and H are operands of products whose depth is the node rows; X and dY keep their
-// rows' scales there, by whose inverses dG, dU and H are multiplied before they get a scale of their own, a hidden column each.
+// lay their pieces in LDS, and all multiply all of these, each with its own columns of X and dY.  Results lie as they are (a hidden column is a
+// lane's column), so dG, dU and H are operands of products whose depth is the node rows; X and dY keep their rows' scales there, by whose
+// inverses dG, dU and H are multiplied before they get a scale of their own, a hidden column each.
 template <int ACT, int T>
 __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
   __shared__ Shared<6> shared;
@@ -562,8 +563,9 @@ struct Plan {
     parts = tiles(row_tiles, tiles_per_part);
     // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
     // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; eight waves to 32 rows 13.1 to 14.1 throughout (32 through 128: 5.9, 6.5, 11.5 and 8.8 to
-    // 9.6; 256 through 1024: 48, 53, 97 and 76 to 81).  The kernels for more than 256 columns are slower: 2048 rows there.
-    few = !backward && rows <= (kept ? 256 : 2048) && c.F <= kFewMostF;
+    // 9.6; 256 through 1024: 48, 53, 97 and 76 to 81).  The kernels for more than 256 columns take longer for the same rows: 512 rows there (512
+    // through 2048: 185, 187, 369 at 512, 736 at 1024, in tiles 670 to 700; 40 through 512 to 600: 33, 35, 66, 130, in tiles 77 to 81).
+    few = !backward && rows <= (kept ? 256 : 512) && c.F <= kFewMostF;
     // Eight waves to 32 rows instead of one, as long as that is one round of workgroups: two a compute unit forward, one for the gradient of X,
     // of which 256 columns need two for the same rows.  64 through 256, both with the packing of the weights: 13.8 us instead of 18.7 at
     // 4096 rows, 16.1 instead of 19.7 at 16384, 24.7 instead of 20.7 at 32768; the gradient 19.5 instead of 27.7, 28.7 instead of 28.2 and

@@ -78,7 +78,7 @@ def test_every_width_of_four_or_more_hidden_tiles(pipad, F, hidden, Fo, activati
 
 
 @pytest.mark.parametrize("F,hidden,Fo", [(257, 33, 20), (290, 160, 300), (530, 130, 40), (40, 130, 530), (700, 97, 260), (1100, 40, 3), (600, 257, 1060)])
-@pytest.mark.parametrize("n,k", [(2100, 1), (70, 31)])
+@pytest.mark.parametrize("n,k", [(2100, 1), (70, 31), (512, 1), (513, 1)])
 def test_rows_of_more_than_256_columns(pipad, F, hidden, Fo, n, k):
     check(pipad, n, k, F, hidden, Fo, "silu", layout="padded" if F % 4 else "list")
 
