@@ -8,6 +8,11 @@ Matrices are given as for :func:`frame_aggregate`: a list of k float32 [n, F] ma
 tensor.  Results that are not given are allocated in the form of the first operand, a list's k matrices as one piece of memory.
 Calls only enqueue work on the stream.  Plain calls with memory for their results go through the binding's native half (see
 binding.py), which leaves anything else to the code here.  The workspace comes from PyTorch's allocator where none is given.
+
+What a call with ``stream=`` makes (results, gradients, the workspace) is memory of that stream and lives until the work that
+is on the current stream when it is dropped has ended.  As always with PyTorch, the streams have to be ordered by the caller: the
+given one behind what makes the operands, the current one behind the call before results are read; and an operand or a
+workspace of another stream that is dropped early needs ``record_stream``.
 """
 from __future__ import annotations
 
@@ -32,7 +37,7 @@ _pack_ff_grads = struct.Struct("3P3q3P").pack      # pipad_gated_ff_grads_t
 class _Rows:
     """n, k, the device and the width of the first operand; everything else has to go with them."""
 
-    def __init__(self, x: Features, name: str):
+    def __init__(self, x: Features, name: str, stream=None):
         if isinstance(x, torch.Tensor):
             if x.dim() != 3:
                 raise ValueError(f"{name}: a single tensor must have shape [n, k, F]")
@@ -46,6 +51,21 @@ class _Rows:
         if not first.is_cuda:
             raise ValueError(f"{name}: every matrix must be float32 [n, F] on the GPU")
         self.device, self.index = first.device, first.get_device()
+        self.raw, self.side = _current_raw_stream(self.index), None
+        if stream is not None and int(stream.cuda_stream) != self.raw:
+            self.raw = int(stream.cuda_stream)
+            self.side = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.raw, self.device)
+
+    def empty(self, shape, dtype: torch.dtype = torch.float32, returned: bool = True) -> torch.Tensor:
+        """Memory for a call on its stream.  The current stream's would not do for another one: the allocator gives again what has just been
+        given back, which work that is queued on the current stream may still read."""
+        if self.side is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.side):
+            made = torch.empty(shape, dtype=dtype, device=self.device)
+        if returned:
+            made.record_stream(torch.cuda.current_stream(self.device))  # that is where it is read
+        return made
 
     def operand(self, x: Optional[Features], name: str, F: Optional[int] = None):
         """(packed pointers, row stride) of an operand of F columns, or of none."""
@@ -64,8 +84,8 @@ class _Rows:
 
     def room(self, F: int) -> Features:
         if self.wide:
-            return torch.empty((self.n, self.k, F), dtype=torch.float32, device=self.device)
-        return list(torch.empty((self.k, self.n, F), dtype=torch.float32, device=self.device).unbind(0))
+            return self.empty((self.n, self.k, F))
+        return list(self.empty((self.k, self.n, F)).unbind(0))
 
     def vector(self, v: Optional[torch.Tensor], F: int, name: str) -> int:
         if v is None:
@@ -80,13 +100,10 @@ class _Rows:
             raise ValueError(f"{name} must be a float32 [{rows}, {columns}] matrix with unit column stride on the operands' device")
         return w.data_ptr(), w.stride(0) if rows > 1 else max(columns, w.stride(0))
 
-    def call(self, fn, *args, stream=None) -> None:
-        _check(_on_device(self.index, fn, *args, self.stream(stream)))
+    def call(self, fn, *args) -> None:
+        _check(_on_device(self.index, fn, *args, self.raw))
 
-    def stream(self, stream) -> int:
-        return int(stream.cuda_stream) if stream is not None else _current_raw_stream(self.index)
-
-    def workspace(self, given: Optional[torch.Tensor], nbytes: int, stream) -> Tuple[Optional[torch.Tensor], int, int]:
+    def workspace(self, given: Optional[torch.Tensor], nbytes: int) -> Tuple[Optional[torch.Tensor], int, int]:
         """(what to keep until the call is enqueued, its address, its bytes)"""
         if given is not None:
             if given.get_device() != self.index or not given.is_contiguous():
@@ -94,9 +111,7 @@ class _Rows:
             return given, given.data_ptr(), given.numel() * given.element_size()
         if not nbytes:
             return None, 0, 0
-        made = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        if stream is not None and int(stream.cuda_stream) != _current_raw_stream(self.index):
-            made.record_stream(stream)  # it goes back in the order of the current stream otherwise
+        made = self.empty(nbytes, torch.uint8, returned=False)
         return made, made.data_ptr(), nbytes
 
 
@@ -160,7 +175,7 @@ def residual_norm(R: Features, B: Optional[Features] = None, gate: Optional[Feat
             if status:
                 _check(status)
             return (R if B is None else R_out), Z
-    rows = _Rows(R, "R")
+    rows = _Rows(R, "R", stream)
     F = rows.width(R)
     r = rows.operand(R, "R")
     norm = _norm_struct(rows, F, post, pre, eps, scale, w_post, b_post, w_pre, b_pre)
@@ -169,7 +184,7 @@ def residual_norm(R: Features, B: Optional[Features] = None, gate: Optional[Feat
     if pre is not None and Z is None:
         Z = rows.room(F)
     rows.call(lib.pipad_residual_norm, norm, rows.n, rows.k, *r, *rows.operand(B, "B", F), *rows.operand(gate, "gate", F),
-              *rows.operand(R_out, "R_out", F), *rows.operand(Z, "Z", F), stream=stream)
+              *rows.operand(R_out, "R_out", F), *rows.operand(Z, "Z", F))
     return (R if B is None else R_out), Z
 
 
@@ -195,7 +210,7 @@ def residual_norm_backward(R: Features, dR_out: Optional[Features] = None, dZ: O
             if made[0]:
                 _check(made[0])
             return ResidualNormGrads(dR, dB, dgate, *made[1:])
-    rows = _Rows(R, "R")
+    rows = _Rows(R, "R", stream)
     F = rows.width(R)
     r = rows.operand(R, "R")
     norm = _norm_struct(rows, F, post, pre, eps, scale, w_post, b_post, w_pre, None)
@@ -205,16 +220,16 @@ def residual_norm_backward(R: Features, dR_out: Optional[Features] = None, dZ: O
         dB = rows.room(F)
     if gate is not None and dgate is None:
         dgate = rows.room(F)
-    grads = [torch.empty(F, dtype=torch.float32, device=rows.device) if w else None for w in wanted]
+    grads = [rows.empty(F) if w else None for w in wanted]
     packed, kept, ws = None, None, (0, 0)
     if any(wanted):
         packed = _pack_norm_grads(*[0 if d is None else d.data_ptr() for d in grads])
         need = _size_t()
         _check(lib.pipad_residual_norm_workspace(F, rows.n, rows.k, ctypes.byref(need)))
-        kept, *ws = rows.workspace(workspace, need.value, stream)
+        kept, *ws = rows.workspace(workspace, need.value)
     rows.call(lib.pipad_residual_norm_backward, norm, rows.n, rows.k, *r, *rows.operand(B, "B", F), *rows.operand(gate, "gate", F),
               *rows.operand(dR_out, "dR_out", F), *rows.operand(dZ, "dZ", F), *rows.operand(dR, "dR", F), *rows.operand(dB, "dB", F),
-              *rows.operand(dgate, "dgate", F), packed, *ws, stream=stream)
+              *rows.operand(dgate, "dgate", F), packed, *ws)
     return ResidualNormGrads(dR, dB, dgate, *grads)
 
 
@@ -258,7 +273,7 @@ def gated_ff(X: Features, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, 
             if status:
                 _check(status)
             return Y
-    rows = _Rows(X, "X")
+    rows = _Rows(X, "X", stream)
     F = rows.width(X)
     x = rows.operand(X, "X")
     block, _, Fo = _ff_struct(rows, F, Wg, Wu, Wd, bg, bu, bd, activation)
@@ -266,8 +281,8 @@ def gated_ff(X: Features, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, 
         Y = rows.room(Fo)
     need = _size_t()
     _check(lib.pipad_gated_ff_workspace(block, rows.n, rows.k, 0, ctypes.byref(need)))
-    kept, *ws = rows.workspace(workspace, need.value, stream)
-    rows.call(lib.pipad_gated_ff, block, rows.n, rows.k, *x, *rows.operand(Y, "Y", Fo), *ws, stream=stream)
+    kept, *ws = rows.workspace(workspace, need.value)
+    rows.call(lib.pipad_gated_ff, block, rows.n, rows.k, *x, *rows.operand(Y, "Y", Fo), *ws)
     return Y
 
 
@@ -289,7 +304,7 @@ def gated_ff_backward(X: Features, dY: Features, Wg: torch.Tensor, Wu: torch.Ten
             if made[0]:
                 _check(made[0])
             return GatedFFGrads(dX if rows_grad else None, *made[1:])
-    rows = _Rows(X, "X")
+    rows = _Rows(X, "X", stream)
     F = rows.width(X)
     x = rows.operand(X, "X")
     block, hidden, Fo = _ff_struct(rows, F, Wg, Wu, Wd, bg, bu, None, activation)
@@ -300,13 +315,13 @@ def gated_ff_backward(X: Features, dY: Features, Wg: torch.Tensor, Wu: torch.Ten
         dX = rows.room(F)
     shapes = [(F, hidden), (F, hidden), (hidden, Fo)] if weights else [None] * 3
     shapes += [(hidden,), (hidden,), (Fo,)] if biases else [None] * 3
-    grads = [None if s is None else torch.empty(s, dtype=torch.float32, device=rows.device) for s in shapes]
+    grads = [None if s is None else rows.empty(s) for s in shapes]
     packed = None
     if weights or biases:
         at = [0 if d is None else d.data_ptr() for d in grads]
         packed = _pack_ff_grads(*at[:3], hidden, hidden, Fo, *at[3:])
     need = _size_t()
     _check(lib.pipad_gated_ff_workspace(block, rows.n, rows.k, 1, ctypes.byref(need)))
-    kept, *ws = rows.workspace(workspace, need.value, stream)
-    rows.call(lib.pipad_gated_ff_backward, block, rows.n, rows.k, *x, *dy, *rows.operand(dX, "dX", F), packed, *ws, stream=stream)
+    kept, *ws = rows.workspace(workspace, need.value)
+    rows.call(lib.pipad_gated_ff_backward, block, rows.n, rows.k, *x, *dy, *rows.operand(dX, "dX", F), packed, *ws)
     return GatedFFGrads(dX, *grads)
