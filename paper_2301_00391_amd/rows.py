@@ -27,6 +27,7 @@ from .binding import MAX_K, Features, _address, _check, _current_device, _curren
 
 _NORMS = {None: 0, "rms": 1, "layer": 2}
 _ACTIVATIONS = {"sigmoid": 0, "relu": 1, "gelu": 2, "silu": 3}
+_MOST_ROWS, _TOO_LARGE = 2 ** 31 - 1, -4           # (ctypes would pass on the low 32 bits)
 _size_t = ctypes.c_size_t
 _pack_norm = struct.Struct("iiif5P").pack          # pipad_residual_norm_t
 _pack_norm_grads = struct.Struct("5P").pack        # pipad_residual_norm_grads_t
@@ -48,6 +49,8 @@ class _Rows:
             self.n, self.k, self.wide, first = x[0].shape[0], len(x), False, x[0]
         if not 1 <= self.k <= MAX_K:
             raise ValueError(f"{name}: need 1 to {MAX_K} matrices [n, F]")
+        if self.n > _MOST_ROWS:
+            _check(_TOO_LARGE)
         if not first.is_cuda:
             raise ValueError(f"{name}: every matrix must be float32 [n, F] on the GPU")
         self.device, self.index = first.device, first.get_device()
