@@ -218,7 +218,9 @@ __device__ inline float2 activate_slope(float x) {
     const Normal p = normal_of(x);
     return make_float2(fmaf(-fabsf(x), p.tail, relu_of(x)), fmaf(x * 0.39894228f, p.density, x < 0.f ? p.tail : 1.f - p.tail));
   }
-  const float s = __builtin_amdgcn_rcpf(1.f + __expf(-x)), rest = 1.f - s;
+  // 1 - s = exp(-x) s: the difference would lose it where the gate is wide open.  Where the exponential has no end, s is 0 and the product is no
+  // number, of which the least is 1.
+  const float e = __expf(-x), s = __builtin_amdgcn_rcpf(1.f + e), rest = fminf(e * s, 1.f);
   if (ACT == PIPAD_ACT_SIGMOID) return make_float2(s, s * rest);
   const float a = x * s;
   return make_float2(a, fmaf(a, rest, s));
