@@ -179,10 +179,10 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
 // store: no launch for fragments, and every wave has its loads on the way at once.  Columns lie along the lanes; the sum over the rows
 // of a matrix is shared by as many waves as there are left, and added up in LDS, always in the same order.  One row of 64 through 256: 7.5 us, of which a
 // launch and two round trips to memory are most (13.1 with fragments and eight waves).
-constexpr int kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewColumns = 1024, kFewMostF = 2048;
+constexpr int kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewColumns = 1024, kFewMostF = 2048, kFewMostFo = 8192;
 template <int ACT>
 __global__ void __launch_bounds__(kFewThreads) k_ff_few(FfArgs a) {
-  __shared__ float x[kFewMostF], sum_g[kFewThreads], sum_u[kFewThreads], hidden[kFewColumns];
+  __shared__ float x[kFewMostF], sum_g[kFewThreads], sum_u[kFewThreads], hidden[kFewColumns], sums[kFewMostFo];  // (sums: of more than kFewColumns hidden columns)
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const RowAt at = row_at(a, blockIdx.x, 0);
   const float *const row = a.X[at.t] + at.i * a.ldx;
@@ -224,9 +224,10 @@ __global__ void __launch_bounds__(kFewThreads) k_ff_few(FfArgs a) {
       __syncthreads();
       if (threadIdx.x < outs) {
         const int o = o0 + threadIdx.x;
-        float s = h0 ? out[o] : a.bd_in ? a.bd_in[o] : 0.f;
+        float s = h0 ? sums[o] : a.bd_in ? a.bd_in[o] : 0.f;
         for (int q = 0; q < ogroups; ++q) s += sum_g[q * oblocks * kWave + threadIdx.x];
-        out[o] = s;
+        if (h0 + kFewColumns < a.hidden) sums[o] = s;
+        else out[o] = s;
       }
       __syncthreads();
     }
@@ -565,7 +566,7 @@ struct Plan {
     // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; eight waves to 32 rows 13.1 to 14.1 throughout (32 through 128: 5.9, 6.5, 11.5 and 8.8 to
     // 9.6; 256 through 1024: 48, 53, 97 and 76 to 81).  The kernels for more than 256 columns take longer for the same rows: 512 rows there (512
     // through 2048: 185, 187, 369 at 512, 736 at 1024, in tiles 670 to 700; 40 through 512 to 600: 33, 35, 66, 130, in tiles 77 to 81).
-    few = !backward && rows <= (kept ? 256 : 512) && c.F <= kFewMostF;
+    few = !backward && rows <= (kept ? 256 : 512) && c.F <= kFewMostF && (c.hidden <= kFewColumns || c.Fo <= kFewMostFo);  // (LDS holds a row, its sums)
     // Eight waves to 32 rows instead of one, as long as that is one round of workgroups: two a compute unit forward, one for the gradient of X,
     // of which 256 columns need two for the same rows.  64 through 256, both with the packing of the weights: 13.8 us instead of 18.7 at
     // 4096 rows, 16.1 instead of 19.7 at 16384, 24.7 instead of 20.7 at 32768; the gradient 19.5 instead of 27.7, 28.7 instead of 28.2 and
