@@ -14,12 +14,13 @@
 // kernels: 8 million rows of 64 through 171 columns took 2.85 ms with them and take 2.08 now.
 //
 // A 16-bit float reaches from 2^-24 to 2^16, so operands are scaled, by powers of two: rows of X and dY by their largest value, weights by the
-// largest of the block that goes with 32 hidden columns, H, dG and dU by the largest of a node's (or in the weights' gradients a hidden column's)
-// 32 values at a time, whose products are added up outside.  Largest values come to 2^14 .. 2^15.  Two forms:
-//  - wide, for X, dY and their partners forward and in the gradient of X: h2 is kept 2^11 larger and its products are summed apart, so that
-//    values down to 2^-29 of the largest have all their bits, and smaller ones an error of 2^-51 of it;
-//  - narrow, for H, dG and dU in the products with weights, and in the weights' gradients throughout, which the additions to two sums bound:
-//    h2 as it is, one sum; all bits down to 2^-18 of the largest, an error of 2^-40 of it below.
+// largest of the column that a result sees (Wg's and Wu's columns for G and U, Wd's rows for dH, Wd's columns for Y, and for dX the rows of Wg and
+// Wu, which share one), so that a huge or infinite weight is a matter of its own column; H, dG and dU by the largest of a node's (or in the weights'
+// gradients a hidden column's) 32 values at a time, whose products are added up outside.  Largest values come to 2^14 .. 2^15.  Two forms:
+//  - wide, forward and in the gradient of X: h2 is kept 2^11 larger and its products are summed apart, so that values down to 2^-29 of the
+//    largest have all their bits, and smaller ones an error of 2^-51 of it;
+//  - narrow, in the weights' gradients, which the additions to two sums bound: h2 as it is, one sum; all bits down to 2^-18 of the largest, an
+//    error of 2^-40 of it below.
 // A value that is not finite makes its row NaN (or infinite).
 //
 // An instruction aligns what it adds to the largest of it and cuts off, so a sum comes out low by some 1e-8 of its terms' size; over millions of
@@ -49,7 +50,7 @@ constexpr float kWide = 2048.f;       // what h2 is multiplied by in the wide fo
 __host__ __device__ constexpr int gu_words(int fq) { return fq * 2 * kFragment + kWave; }
 struct TileVectors {
   float bg[kTile], bu[kTile];
-  float inv_gu, inv_up, inv_down, inv_back;  // 1 over the scales of the tile's weights
+  float inv_g[kTile], inv_u[kTile], inv_d[kTile];  // 1 over the scales of Wg's and Wu's columns, and of Wd's rows
 };
 static_assert(sizeof(TileVectors) <= kWave * sizeof(u32x4), "fits behind the fragments");
 
@@ -93,18 +94,19 @@ struct Split {
 };
 template <bool WIDE>
 __device__ inline Split split8(const float (&v)[8], float scale) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
   typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  constexpr float kBy = WIDE ? kWide : 1.f;
+  const float by = scale * kBy;
   Split s;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float a = v[2 * i] * scale, b = v[2 * i + 1] * scale;
-    const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
-    a -= (float)h[0];
-    b -= (float)h[1];
-    if (WIDE) a *= kWide, b *= kWide;
-    s.p[0][i] = __builtin_bit_cast(uint32_t, h);
-    s.p[1][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
+    // (as multiply-adds that take and give 16 bits, and in one register from there on: three and a half instructions a value)
+    uint32_t both = __builtin_bit_cast(uint32_t, (f16x2{(_Float16)fmaf(v[2 * i], scale, 0.f), (_Float16)fmaf(v[2 * i + 1], scale, 0.f)}));
+    asm("" : "+v"(both));
+    const f16x2 h = __builtin_bit_cast(f16x2, both);
+    const f16x2 rest{(_Float16)fmaf((float)h[0], -kBy, v[2 * i] * by), (_Float16)fmaf((float)h[1], -kBy, v[2 * i + 1] * by)};
+    s.p[0][i] = both;
+    s.p[1][i] = __builtin_bit_cast(uint32_t, rest);
   }
   return s;
 }
@@ -119,12 +121,6 @@ __device__ inline f32x16 zeros() {
 __device__ inline f32x16 mfma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-// c + a b, both narrow, the small products first
-__device__ inline f32x16 product(const Split &a, const Split &b, f32x16 c) {
-  c = mfma(a.p[1], b.p[0], c);
-  c = mfma(a.p[0], b.p[1], c);
-  return mfma(a.p[0], b.p[0], c);
-}
 struct Sums {  // of wide products: main + cross / kWide
   f32x16 main, cross;
 };
@@ -138,39 +134,44 @@ __device__ inline Split fragment(const u32x4 *at, int64_t index) {
   at += index * kFragment + (threadIdx.x & (kWave - 1));
   return Split{{at[0], at[kWave]}};
 }
-// The sums times what was divided out, and a vector with one value a row of the result.
-__device__ inline f32x16 value_of(const Sums &c, float inv, const float *per_row, int g) {
+// The sums times what was divided out, of the result's column and of its row, and a vector with one value a row.
+__device__ inline float sum_of(const Sums &c, int r) { return fmaf(c.cross[r], 1.f / kWide, c.main[r]); }
+__device__ inline f32x16 value_of(const Sums &c, float inv, const float *inv_row, const float *per_row, int g) {
   f32x16 z;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const float4 t = *reinterpret_cast<const float4 *>(per_row + 8 * q + 4 * g);
-    const float b[4] = {t.x, t.y, t.z, t.w};
+    const float4 t = *reinterpret_cast<const float4 *>(per_row + 8 * q + 4 * g), u = *reinterpret_cast<const float4 *>(inv_row + 8 * q + 4 * g);
+    const float b[4] = {t.x, t.y, t.z, t.w}, f[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[4 * q + e] = fmaf(c.main[4 * q + e], inv, fmaf(c.cross[4 * q + e], inv * (1.f / kWide), b[e]));
+    for (int e = 0; e < 4; ++e) z[4 * q + e] = fmaf(sum_of(c, 4 * q + e), inv * f[e], b[e]);
   }
   return z;
 }
-__device__ inline f32x16 value_of(const Sums &c, float inv) {
+__device__ inline f32x16 value_of(const Sums &c, float inv, const float *inv_row, int g) {
   f32x16 z;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) z[r] = fmaf(c.main[r], inv, c.cross[r] * (inv * (1.f / kWide)));
+  for (int q = 0; q < 4; ++q) {
+    const float4 u = *reinterpret_cast<const float4 *>(inv_row + 8 * q + 4 * g);
+    const float f[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[4 * q + e] = sum_of(c, 4 * q + e) * (inv * f[e]);
+  }
   return z;
 }
-__device__ inline void add(f32x16 &c, float factor, const f32x16 &x) {
+__device__ inline void add(f32x16 &c, float factor, const Sums &x) {
 #pragma unroll
-  for (int r = 0; r < 16; ++r) c[r] = fmaf(factor, x[r], c[r]);
+  for (int r = 0; r < 16; ++r) c[r] = fmaf(factor, sum_of(x, r), c[r]);
 }
 __device__ inline float largest_of(const f32x16 &x, float so_far = 0.f) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) so_far = max_of(so_far, x[r]);
   return so_far;
 }
-template <bool WIDE>
-__device__ inline Split half(const f32x16 &r, int s, float scale) {  // the registers 8 s .. 8 s + 7 as an operand
+__device__ inline Split half(const f32x16 &r, int s, float scale) {  // the registers 8 s .. 8 s + 7 as a wide operand
   float v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = r[8 * s + j];
-  return split8<WIDE>(v, scale);
+  return split8<true>(v, scale);
 }
 
 // A sum of many terms that carries what the additions round off (over thousands of tiles a plain one is off by more than 1e-6).
@@ -234,11 +235,11 @@ struct FfArgs {
   int32_t n, k, F, hidden, Fo;
   int32_t ht, fq, oq, ft, ot;  // 32-column tiles of the hidden columns, 16- and 32-column tiles of X's and Y's
   bool vec_x, vec_dy, vec_o;
-  // Weights as fragments.  gu, wide: [ht], each [fq][Wg, Wu], m = hidden column, depth = X's columns, and a TileVectors behind them.
-  // up, wide: [ht][oq], m = hidden, depth = Y's columns (Wd).  down, narrow: [ht][ot][2], m = Y's column, depth of a result = hidden.
-  // back, narrow: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
+  // Weights as fragments, all wide.  gu: [ht], each [fq][Wg, Wu], m = hidden column, depth = X's columns, and a TileVectors behind them.
+  // up: [ht][oq], m = hidden, depth = Y's columns (Wd).  down: [ht][ot][2], m = Y's column, depth of a result = hidden.
+  // back: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
   const u32x4 *gu, *down, *up, *back;
-  const float *bd;  // padded with zeros to whole tiles
+  const float *inv_out, *bd;  // 1 over the scales of down's or back's columns, and bd; padded to whole tiles
   const float *Wg, *Wu, *Wd, *bg, *bu, *bd_in;  // as they came
   int64_t ldwg, ldwu, ldwd;
   // weight gradients: partial sums of `parts` ranges of rows, each [dWg F x hidden | dWu | dWd hidden x Fo | dbg | dbu | dbd]
@@ -292,6 +293,14 @@ __device__ inline f32x16 per_row(const float *p, int g) {
     const float4 t = *reinterpret_cast<const float4 *>(p + 8 * q + 4 * g);
     z[4 * q] = t.x, z[4 * q + 1] = t.y, z[4 * q + 2] = t.z, z[4 * q + 3] = t.w;
   }
+  return z;
+}
+// Y's or dX's columns c0 .. as they are: times 1 over their scales, and Y's bias.
+__device__ inline f32x16 unscaled(const f32x16 &sums, const float *inv, const float *bias, int g) {
+  f32x16 z = per_row(inv, g), b = zeros();
+  if (bias) b = per_row(bias, g);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = fmaf(sums[r], z[r], b[r]);
   return z;
 }
 // A result's rows are columns c0 .. of a matrix, its column m a row of it.

@@ -17,88 +17,150 @@ struct PackArgs {
   int64_t ldwg, ldwu, ldwd;
   int32_t F, hidden, Fo, ht, fq, oq, ft, ot;
   u32x4 *gu, *down, *up, *back;  // (all but gu: null where they are not wanted)
-  float *pbd;
+  float *inv_out, *pbd;          // (pbd with down only)
+  int32_t tiles;                 // hidden tiles that a workgroup has of down or back
 };
-// A workgroup a hidden tile: the largest of its weights, then a wave a fragment.
+// A workgroup a hidden tile (gu, up) or, behind these, some hidden tiles of 32 columns of Y (down) or X (back): the largest of each column, then a
+// wave a fragment.  What a fragment's m is has a scale of its own, the lane's.
 constexpr int kPackWaves = 16;
-__global__ void __launch_bounds__(kPackWaves *kWave) k_ff_pack(PackArgs a) {
-  __shared__ float found[2][kPackWaves];
-  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int h = blockIdx.x, h0 = h * kTile;
-  {
-    float gu = 0.f, down = 0.f;
-    if (h0 + m < a.hidden)
-      for (int f = 2 * wave + g; f < a.F; f += 2 * kPackWaves) gu = max_of(max_of(gu, a.Wg[f * a.ldwg + h0 + m]), a.Wu[f * a.ldwu + h0 + m]);
-    for (int r = h0 + wave; r < a.hidden && r < h0 + kTile; r += kPackWaves)
-      for (int c = lane; c < a.Fo; c += kWave) down = max_of(down, a.Wd[r * a.ldwd + c]);
-    gu = max_of_wave(gu), down = max_of_wave(down);
-    if (lane == 0) found[0][wave] = gu, found[1][wave] = down;
-  }
-  __syncthreads();
-  float gu = 0.f, down = 0.f;
-#pragma unroll
-  for (int w = 0; w < kPackWaves; ++w) gu = fmaxf(gu, found[0][w]), down = fmaxf(down, found[1][w]);
-  const Scale scale_gu = scale_for(gu), scale_down = scale_for(down);
-  u32x4 *const tile = a.gu + (int64_t)h * gu_words(a.fq);
-  if (threadIdx.x < kWave) {
-    TileVectors &t = *reinterpret_cast<TileVectors *>(tile + a.fq * 2 * kFragment);
-    const float *const b = g ? a.bu : a.bg;
-    (g ? t.bu : t.bg)[m] = b && h0 + m < a.hidden ? b[h0 + m] : 0.f;
-    if (lane == 0) t.inv_gu = t.inv_back = scale_gu.inv, t.inv_up = t.inv_down = scale_down.inv;
-  }
-  if (h == 0)
-    for (int c = threadIdx.x; c < a.ot * kTile; c += kPackWaves * kWave) a.pbd[c] = a.bd && c < a.Fo ? a.bd[c] : 0.f;
 
-  const int n_gu = 2 * a.fq, n_down = a.down ? 2 * a.ot : 0, n_up = a.up ? a.oq : 0, n_back = a.back ? 4 * a.ft : 0;
-  for (int at = wave; at < n_gu + n_down + n_up + n_back; at += kPackWaves) {
+// Largest of the columns c0 .. c0 + 31 of N matrices, column m in lanes m and m + 32, of this wave's rows.
+template <int N>
+__device__ inline void largest_of_columns(float (&x)[N], const float *const (&W)[N], const int64_t (&ld)[N], int rows, int c, bool there, int wave, int g) {
+#pragma unroll
+  for (int q = 0; q < N; ++q) x[q] = 0.f;
+  if (there) {
+#pragma unroll 4
+    for (int r = 2 * wave + g; r < rows; r += 2 * kPackWaves)
+#pragma unroll
+      for (int q = 0; q < N; ++q) x[q] = max_of(x[q], W[q][r * ld[q] + c]);
+  }
+#pragma unroll
+  for (int q = 0; q < N; ++q) x[q] = max_over_32(x[q]);
+}
+// Largest of rows `wave` and `wave` + 16 of 32 in N matrices together; behind the last row the last one's (no branch: all loads are on the way at once).
+template <int N>
+__device__ inline void largest_of_rows(float (&to)[kTile], const float *const (&W)[N], const int64_t (&ld)[N], int first, int rows, int columns, int lane, int wave) {
+  float x[2] = {0.f, 0.f};
+  const int64_t r[2] = {min(first + wave, rows - 1), min(first + wave + kPackWaves, rows - 1)};
+#pragma unroll 4
+  for (int c = lane; c < columns; c += kWave)
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int q = 0; q < N; ++q) x[s] = max_of(x[s], W[q][r[s] * ld[q] + c]);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    x[s] = max_of_wave(x[s]);
+    if (lane == 0) to[wave + s * kPackWaves] = x[s];
+  }
+}
+
+// The scales of m's column, of what the waves have found.
+__device__ inline Scale scale_of(const float (&found)[kPackWaves][kTile], int m) {
+  float x = 0.f;
+#pragma unroll
+  for (int w = 0; w < kPackWaves; ++w) x = fmaxf(x, found[w][m]);
+  return scale_for(x);
+}
+
+__device__ inline void pack_hidden(const PackArgs &a, int h, float (&found)[2][kPackWaves][kTile], float (&rows)[kTile]) {
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int h0 = h * kTile;
+  const bool there = h0 + m < a.hidden;
+  float largest[2];
+  largest_of_columns<2>(largest, {a.Wg, a.Wu}, {a.ldwg, a.ldwu}, a.F, h0 + m, there, wave, g);
+  if (g == 0) found[0][wave][m] = largest[0], found[1][wave][m] = largest[1];
+  if (a.up) largest_of_rows<1>(rows, {a.Wd}, {a.ldwd}, h0, a.hidden, a.Fo, lane, wave);
+  __syncthreads();
+  const Scale scale_g = scale_of(found[0], m), scale_u = scale_of(found[1], m), scale_d = scale_for(a.up ? rows[m] : 0.f);
+  u32x4 *const tile = a.gu + (int64_t)h * gu_words(a.fq);
+  if (threadIdx.x < kTile) {
+    TileVectors &t = *reinterpret_cast<TileVectors *>(tile + a.fq * 2 * kFragment);
+    t.bg[m] = a.bg && there ? a.bg[h0 + m] : 0.f;
+    t.bu[m] = a.bu && there ? a.bu[h0 + m] : 0.f;
+    t.inv_g[m] = scale_g.inv, t.inv_u[m] = scale_u.inv, t.inv_d[m] = scale_d.inv;
+  }
+  const int n_gu = 2 * a.fq, n_up = a.up ? a.oq : 0;
+  for (int at = wave; at < n_gu + n_up; at += kPackWaves) {
     float v[8];
     Split s;
     u32x4 *to;
-    int q = at;
-    if (q < n_gu) {  // [fq][Wg, Wu]
-      const float *W = q % 2 ? a.Wu : a.Wg;
-      const int64_t ld = q % 2 ? a.ldwu : a.ldwg;
+    if (at < n_gu) {  // [fq][Wg, Wu]
+      const float *W = at % 2 ? a.Wu : a.Wg;
+      const int64_t ld = at % 2 ? a.ldwu : a.ldwg;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int f = q / 2 * kDepth + 8 * g + j;
-        v[j] = f < a.F && h0 + m < a.hidden ? W[f * ld + h0 + m] : 0.f;
+        const int f = at / 2 * kDepth + 8 * g + j;
+        v[j] = f < a.F && there ? W[f * ld + h0 + m] : 0.f;
       }
-      s = split8<true>(v, scale_gu.to);
-      to = tile + q * kFragment;
-    } else if ((q -= n_gu) < n_down) {  // [ot][2]
-      const int fo = q / 2 * kTile + m;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int hid = h0 + result_depth(q % 2, g, j);
-        v[j] = hid < a.hidden && fo < a.Fo ? a.Wd[hid * a.ldwd + fo] : 0.f;
-      }
-      s = split8<false>(v, scale_down.to);
-      to = a.down + ((int64_t)h * n_down + q) * kFragment;
-    } else if ((q -= n_down) < n_up) {  // [oq]
-      if (h0 + m < a.hidden) {
-        load8(v, a.Wd + (h0 + m) * a.ldwd, q * kDepth + 8 * g, a.Fo, false);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.f;
-      }
-      s = split8<true>(v, scale_down.to);
-      to = a.up + ((int64_t)h * n_up + q) * kFragment;
-    } else {  // [ft][2][Wg, Wu]
-      q -= n_up;
-      const int f = q / 4 * kTile + m;
-      const float *W = q % 2 ? a.Wu : a.Wg;
-      const int64_t ld = q % 2 ? a.ldwu : a.ldwg;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int hid = h0 + result_depth(q / 2 % 2, g, j);
-        v[j] = hid < a.hidden && f < a.F ? W[f * ld + hid] : 0.f;
-      }
-      s = split8<false>(v, scale_gu.to);
-      to = a.back + ((int64_t)h * n_back + q) * kFragment;
+      s = split8<true>(v, at % 2 ? scale_u.to : scale_g.to);
+      to = tile + at * kFragment;
+    } else {  // [oq]
+      load8(v, a.Wd + (there ? h0 + m : 0) * a.ldwd, (at - n_gu) * kDepth + 8 * g, there ? a.Fo : 0, false);
+      s = split8<true>(v, scale_d.to);
+      to = a.up + ((int64_t)h * n_up + at - n_gu) * kFragment;
     }
 #pragma unroll
     for (int p = 0; p < 2; ++p) to[p * kWave + lane] = s.p[p];
   }
+}
+
+__device__ inline void pack_down(const PackArgs &a, int o, int first, float (&found)[kPackWaves][kTile]) {
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int c = o * kTile + m;
+  const bool there = c < a.Fo;
+  float largest[1];
+  largest_of_columns<1>(largest, {a.Wd}, {a.ldwd}, a.hidden, c, there, wave, g);
+  if (g == 0) found[wave][m] = largest[0];
+  __syncthreads();
+  const Scale scale = scale_of(found, m);
+  if (first == 0 && threadIdx.x < kTile) a.inv_out[c] = scale.inv, a.pbd[c] = a.bd && there ? a.bd[c] : 0.f;
+  const int count = 2 * min(a.ht - first, a.tiles);
+  for (int at = wave; at < count; at += kPackWaves) {  // [2]
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int hid = (first + at / 2) * kTile + result_depth(at % 2, g, j);
+      v[j] = hid < a.hidden && there ? a.Wd[hid * a.ldwd + c] : 0.f;
+    }
+    const Split s = split8<true>(v, scale.to);
+    u32x4 *const to = a.down + (((int64_t)(first + at / 2) * a.ot + o) * 2 + at % 2) * kFragment;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) to[p * kWave + lane] = s.p[p];
+  }
+}
+
+__device__ inline void pack_back(const PackArgs &a, int t, int first, float (&rows)[kTile]) {
+  const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int f = t * kTile + m;
+  largest_of_rows<2>(rows, {a.Wg, a.Wu}, {a.ldwg, a.ldwu}, t * kTile, a.F, a.hidden, lane, wave);
+  __syncthreads();
+  const Scale scale = scale_for(rows[m]);
+  if (first == 0 && threadIdx.x < kTile) a.inv_out[f] = scale.inv;
+  const int count = 4 * min(a.ht - first, a.tiles);
+  for (int at = wave; at < count; at += kPackWaves) {  // [2][Wg, Wu]
+    const float *W = at % 2 ? a.Wu : a.Wg;
+    const int64_t ld = at % 2 ? a.ldwu : a.ldwg;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int hid = (first + at / 4) * kTile + result_depth(at / 2 % 2, g, j);
+      v[j] = hid < a.hidden && f < a.F ? W[f * ld + hid] : 0.f;
+    }
+    const Split s = split8<true>(v, scale.to);
+    u32x4 *const to = a.back + (((int64_t)(first + at / 4) * a.ft + t) * 4 + at % 4) * kFragment;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) to[p * kWave + lane] = s.p[p];
+  }
+}
+
+__global__ void __launch_bounds__(kPackWaves *kWave) k_ff_pack(PackArgs a) {
+  __shared__ float found[2][kPackWaves][kTile], rows[kTile];
+  const int b = (int)blockIdx.x - a.ht;
+  if (b < 0) return pack_hidden(a, blockIdx.x, found, rows);
+  if (a.down) return pack_down(a, b % a.ot, b / a.ot * a.tiles, found[0]);
+  pack_back(a, b % a.ft, b / a.ft * a.tiles, rows);
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -133,7 +195,7 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
   const int o0 = (blockIdx.y * kWavesPerBlock + wave) * OT;
   f32x16 y[OT];
 #pragma unroll
-  for (int o = 0; o < OT; ++o) y[o] = o0 + o < a.ot ? per_row(a.bd + (o0 + o) * kTile, g) : zeros();
+  for (int o = 0; o < OT; ++o) y[o] = zeros();
   for (int h0 = 0, turn = 0; h0 < a.ht; h0 += kWavesPerBlock, turn ^= 1) {
     if (h0 + wave < a.ht) {
       const u32x4 *const gu = a.gu + (int64_t)(h0 + wave) * gu_words(a.fq);
@@ -146,15 +208,14 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
         add_product(sg, fragment(gu, 2 * q), b);
         add_product(su, fragment(gu, 2 * q + 1), b);
       }
-      const float inv = scale_x.inv * vectors.inv_gu;
-      f32x16 G = value_of(sg, inv, vectors.bg, g);
-      const f32x16 U = value_of(su, inv, vectors.bu, g);
+      f32x16 G = value_of(sg, scale_x.inv, vectors.inv_g, vectors.bg, g);
+      const f32x16 U = value_of(su, scale_x.inv, vectors.inv_u, vectors.bu, g);
 #pragma unroll
       for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
       const Scale scale = scale_for(max_over_32(largest_of(G)));
 #pragma unroll
-      for (int s = 0; s < 2; ++s) lay(hs.piece[turn][wave], s, half<false>(G, s, scale.to), lane);
-      hs.inv[turn][wave][lane] = scale.inv * vectors.inv_down;
+      for (int s = 0; s < 2; ++s) lay(hs.piece[turn][wave], s, half(G, s, scale.to), lane);
+      hs.inv[turn][wave][lane] = scale.inv;
     }
     __syncthreads();
     const int count = min(a.ht - h0, kWavesPerBlock);
@@ -165,14 +226,18 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
       for (int o = 0; o < OT; ++o)
         if (o0 + o < a.ot) {
           const int64_t at_w = ((int64_t)(h0 + w) * a.ot + o0 + o) * 2;
-          add(y[o], inv, product(fragment(a.down, at_w + 1), b[1], product(fragment(a.down, at_w), b[0], zeros())));
+          Sums sum = no_sums();
+#pragma unroll
+          for (int s = 0; s < 2; ++s) add_product(sum, fragment(a.down, at_w + s), b[s]);
+          add(y[o], inv, sum);
         }
     }
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
 #pragma unroll
-  for (int o = 0; o < OT; ++o) store_tile(y[o], out, (o0 + o) * kTile, a.Fo, a.vec_o, g);
+  for (int o = 0; o < OT; ++o)
+    if (o0 + o < a.ot) store_tile(unscaled(y[o], a.inv_out + (o0 + o) * kTile, a.bd + (o0 + o) * kTile, g), out, (o0 + o) * kTile, a.Fo, a.vec_o, g);
 }
 
 // Few rows: a workgroup a row, in 32-bit floats, straight from the weights as they are.  What counts is the time from the first load to the last
@@ -265,9 +330,8 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
         load8(v, dy, q * kDepth + 8 * g, a.Fo, a.vec_dy);
         add_product(sd, fragment(a.up, (int64_t)h * a.oq + q), split8<true>(v, scale_dy.to));
       }
-      const float inv = scale_x.inv * vectors.inv_gu;
-      f32x16 G = value_of(sg, inv, vectors.bg, g), U = value_of(su, inv, vectors.bu, g);
-      const f32x16 dH = value_of(sd, scale_dy.inv * vectors.inv_up);
+      f32x16 G = value_of(sg, scale_x.inv, vectors.inv_g, vectors.bg, g), U = value_of(su, scale_x.inv, vectors.inv_u, vectors.bu, g);
+      const f32x16 dH = value_of(sd, scale_dy.inv, vectors.inv_d, g);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float2 c = activate_slope<ACT>(G[r]);
@@ -277,10 +341,10 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
       const Scale scale = scale_for(max_over_32(largest_of(U, largest_of(G))));
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        lay(ds.piece[turn][wave], s, half<false>(G, s, scale.to), lane);
-        lay(ds.piece[turn][wave], 2 + s, half<false>(U, s, scale.to), lane);
+        lay(ds.piece[turn][wave], s, half(G, s, scale.to), lane);
+        lay(ds.piece[turn][wave], 2 + s, half(U, s, scale.to), lane);
       }
-      ds.inv[turn][wave][lane] = scale.inv * vectors.inv_back;
+      ds.inv[turn][wave][lane] = scale.inv;
     }
     __syncthreads();
     const int count = min(a.ht - h0, kWavesPerBlock);
@@ -292,11 +356,12 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
 #pragma unroll
       for (int f = 0; f < FT; ++f)
         if (f0 + f < a.ft) {
-          f32x16 sum = zeros();
+          Sums sum = no_sums();
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             const int64_t at_w = (((int64_t)(h0 + w) * a.ft + f0 + f) * 2 + s) * 2;
-            sum = product(fragment(a.back, at_w + 1), du[s], product(fragment(a.back, at_w), dg[s], sum));
+            add_product(sum, fragment(a.back, at_w), dg[s]);
+            add_product(sum, fragment(a.back, at_w + 1), du[s]);
           }
           add(dx[f], inv, sum);
         }
@@ -305,7 +370,8 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
 #pragma unroll
-  for (int f = 0; f < FT; ++f) store_tile(dx[f], out, (f0 + f) * kTile, a.F, a.vec_o, g);
+  for (int f = 0; f < FT; ++f)
+    if (f0 + f < a.ft) store_tile(unscaled(dx[f], a.inv_out + (f0 + f) * kTile, nullptr, g), out, (f0 + f) * kTile, a.F, a.vec_o, g);
 }
 
 // ---- the gradients of the weights ---------------------------------------------------------------
@@ -325,7 +391,7 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
   Total dbg, dbu, dbd[T];
   const u32x4 *const gu = a.gu + (int64_t)h * gu_words(a.fq);
   const TileVectors &vectors = vectors_of(gu, a.fq);
-  const float bg = vectors.bg[m], bu = vectors.bu[m];
+  const float bg = vectors.bg[m], bu = vectors.bu[m], inv_g = vectors.inv_g[m], inv_u = vectors.inv_u[m], inv_d = vectors.inv_d[m];
   const int64_t first = blockIdx.y * a.tiles_per_part * kTile;
   const int64_t end = first + a.tiles_per_part * kTile < a.rows ? first + a.tiles_per_part * kTile : a.rows;
   const auto sign_of = [](int64_t base) { return base / kTile % 2 ? -1.f : 1.f; };
@@ -355,9 +421,9 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
       for (int r = 0; r < 16; ++r) {
         const int d = result_depth(r / 8, g, r % 8);
         const float inv_x = __shfl(scale_x.inv, d), inv_dy = __shfl(scale_dy.inv, d);
-        const float cx = sign * vectors.inv_gu * inv_x, cd = sign * vectors.inv_up * inv_dy;
-        const float2 c = activate_slope<ACT>(fmaf(sg.main[r], cx, fmaf(sg.cross[r], cx * (1.f / kWide), bg)));
-        const float u = fmaf(su.main[r], cx, fmaf(su.cross[r], cx * (1.f / kWide), bu)), e = fmaf(sd.main[r], cd, sd.cross[r] * (cd * (1.f / kWide)));
+        const float sx = sign * inv_x;
+        const float2 c = activate_slope<ACT>(fmaf(sum_of(sg, r), sx * inv_g, bg));
+        const float u = fmaf(sum_of(su, r), sx * inv_u, bu), e = sum_of(sd, r) * (sign * inv_dy * inv_d);
         vg[r] = e * u * c.y;
         vu[r] = e * c.x;
         tile_g += vg[r];
@@ -383,10 +449,6 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
       if (g == 0) to_of[turn][wave][0][m] = sign * scale_x.to, to_of[turn][wave][1][m] = sign * scale_dy.to;
     }
     __syncthreads();
-    const auto add_sums = [&](f32x16 &to, float factor, const Sums &c) {
-      add(to, factor * (1.f / kWide), c.cross);
-      add(to, factor, c.main);
-    };
     for (int w = 0; w < kWavesPerBlock && batch + w * kTile < end; ++w) {
       const int64_t base = batch + w * kTile;
       const u32x4 *const of = shared.piece[turn][w];
@@ -415,8 +477,8 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
             add_product(g_sum, xs, fragment(of, s));
             add_product(u_sum, xs, fragment(of, 2 + s));
           }
-          add_sums(dwg[t], cg, g_sum);
-          add_sums(dwu[t], cu, u_sum);
+          add(dwg[t], cg, g_sum);
+          add(dwu[t], cu, u_sum);
         }
         if (t0 + t < a.ot) {
           Sums d_sum = no_sums();
@@ -427,7 +489,7 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
             for (int j = 0; j < 8; ++j) dbd[t].add(v[j]);
             add_product(d_sum, dys, fragment(of, 4 + s));
           }
-          add_sums(dwd[t], ch, d_sum);
+          add(dwd[t], ch, d_sum);
         }
       }
     }
@@ -526,7 +588,7 @@ int32_t depth_tiles(int32_t F, bool backward) {
 struct Plan {
   int32_t ht, fq, oq, ft, ot;
   int64_t n_gu, n_down, n_up, n_back;
-  size_t gu, down, up, back, bd, partial, total;
+  size_t gu, down, up, back, inv_out, bd, partial, total;
   int64_t rows, part_floats, parts, tiles_per_part;
   bool kept, few, split;
   int weight_waves;
@@ -546,7 +608,7 @@ struct Plan {
     const size_t fragment_bytes = kFragment * sizeof(u32x4);
     gu = take((size_t)ht * gu_words(fq) * sizeof(u32x4)), down = take(n_down * fragment_bytes);
     up = take(n_up * fragment_bytes), back = take(n_back * fragment_bytes);
-    bd = take(ot * kTile * sizeof(float));
+    inv_out = take((backward ? ft : ot) * kTile * sizeof(float)), bd = take(backward ? 0 : ot * kTile * sizeof(float));
     rows = (int64_t)n * k;
     part_floats = 2 * (int64_t)c.F * c.hidden + (int64_t)c.hidden * c.Fo + 2 * (int64_t)c.hidden + c.Fo;
     // Parts of the rows for the weights' gradients.  Rows of any width: a thousand workgroups, a tile of rows a wave at least.  Up to
@@ -593,18 +655,21 @@ FfArgs arguments(const pipad_gated_ff_t &c, const Plan &p, int32_t n, int32_t k,
   a.ht = p.ht, a.fq = p.fq, a.oq = p.oq, a.ft = p.ft, a.ot = p.ot;
   a.gu = reinterpret_cast<const u32x4 *>(ws + p.gu), a.down = reinterpret_cast<const u32x4 *>(ws + p.down);
   a.up = reinterpret_cast<const u32x4 *>(ws + p.up), a.back = reinterpret_cast<const u32x4 *>(ws + p.back);
-  a.bd = reinterpret_cast<const float *>(ws + p.bd);
+  a.inv_out = reinterpret_cast<const float *>(ws + p.inv_out), a.bd = reinterpret_cast<const float *>(ws + p.bd);
   a.Wg = c.Wg, a.Wu = c.Wu, a.Wd = c.Wd, a.bg = c.bg, a.bu = c.bu, a.bd_in = c.bd, a.ldwg = c.ldwg, a.ldwu = c.ldwu, a.ldwd = c.ldwd;
   a.partial = reinterpret_cast<float *>(ws + p.partial), a.part_floats = p.part_floats, a.tiles_per_part = p.tiles_per_part;
   return a;
 }
 
-int pack(const pipad_gated_ff_t &c, const Plan &p, char *ws, hipStream_t st) {
+int pack(const pipad_gated_ff_t &c, const Plan &p, bool dx, char *ws, hipStream_t st) {
   const auto at = [&](size_t offset, int64_t count) { return count ? reinterpret_cast<u32x4 *>(ws + offset) : nullptr; };
+  // A fragment a wave and one round of loads for it, where the hidden tiles are 64 at most; each workgroup looks for the largest of its columns itself.
+  const int32_t most = std::max<int32_t>(p.n_down ? 8 : 4, (int32_t)tiles(p.ht, 16));
   const PackArgs a{c.Wg,   c.Wu,   c.Wd, c.bg, c.bu, c.bd, c.ldwg, c.ldwu, c.ldwd, c.F, c.hidden, c.Fo,
                    p.ht,   p.fq,   p.oq, p.ft, p.ot, at(p.gu, p.n_gu), at(p.down, p.n_down), at(p.up, p.n_up), at(p.back, p.n_back),
-                   reinterpret_cast<float *>(ws + p.bd)};
-  hipLaunchKernelGGL(k_ff_pack, dim3((unsigned)p.ht), dim3(kPackWaves * kWave), 0, st, a);
+                   reinterpret_cast<float *>(ws + p.inv_out), reinterpret_cast<float *>(ws + p.bd), most};
+  const int64_t columns = p.n_down ? p.ot : dx ? p.ft : 0;
+  hipLaunchKernelGGL(k_ff_pack, dim3((unsigned)(p.ht + columns * tiles(p.ht, most))), dim3(kPackWaves * kWave), 0, st, a);
   PIPAD_HIP(hipGetLastError());
   return PIPAD_OK;
 }
@@ -637,7 +702,7 @@ int gated_ff_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float
     PIPAD_HIP(hipGetLastError());
     return PIPAD_OK;
   }
-  const int rc = pack(c, p, ws, st);
+  const int rc = pack(c, p, false, ws, st);
   if (rc != PIPAD_OK) return rc;
   if (p.kept) {
     const Kept f = p.split ? split_forward(c.activation, p.ot) : kept_forward(c.activation, p.fq, p.ot);
@@ -658,7 +723,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
   char *const ws = static_cast<char *>(workspace);
   if (p.rows > 0) {
     // The kernel for the weights' gradients of rows of up to 256 columns reads the weights as they are.
-    const int rc = dX || !p.kept ? pack(c, p, ws, st) : PIPAD_OK;
+    const int rc = dX || !p.kept ? pack(c, p, dX != nullptr, ws, st) : PIPAD_OK;
     if (rc != PIPAD_OK) return rc;
     const FfArgs a = arguments(c, p, n, k, X, ldx, dY, lddy, dX, lddx, ws);
     if (dX && p.kept) {

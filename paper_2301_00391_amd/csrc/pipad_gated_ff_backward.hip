@@ -39,12 +39,11 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_
       add_product(su, fragment(in, 2 * q + 1), x[q]);
     }
     const TileVectors &v = vectors_of(in, FQ);
-    const float inv = inv_x * v.inv_gu, inv_back = v.inv_back;
-    f32x16 G = value_of(sg, inv, v.bg, g), U = value_of(su, inv, v.bu, g);
+    f32x16 G = value_of(sg, inv_x, v.inv_g, v.bg, g), U = value_of(su, inv_x, v.inv_u, v.bu, g);
     Sums sd = no_sums();
 #pragma unroll
     for (int q = 0; q < OQ; ++q) add_product(sd, fragment(in + kGu, q), dy[q]);
-    const f32x16 dH = value_of(sd, inv_dy * v.inv_up);
+    const f32x16 dH = value_of(sd, inv_dy, v.inv_d, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float2 c = activate_slope<ACT>(G[r]);
@@ -52,7 +51,7 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_
       U[r] = dH[r] * c.x;
     }
     const Scale scale = scale_for(max_over_32(largest_of(U, largest_of(G))));
-    const Split dg[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)}, du[2] = {half<false>(U, 0, scale.to), half<false>(U, 1, scale.to)};
+    const Split dg[2] = {half(G, 0, scale.to), half(G, 1, scale.to)}, du[2] = {half(U, 0, scale.to), half(U, 1, scale.to)};
     staged();
     if (h + 1 < a.ht) {
       stage<WAVES, kGu>(a.gu + (int64_t)(h + 1) * kGu, in);
@@ -60,16 +59,19 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_
     }
 #pragma unroll
     for (int f = 0; f < FT; ++f) {
-      f32x16 sum = zeros();
+      Sums sum = no_sums();
 #pragma unroll
-      for (int s = 0; s < 2; ++s) sum = product(fragment(back, (f * 2 + s) * 2 + 1), du[s], product(fragment(back, (f * 2 + s) * 2), dg[s], sum));
-      add(dx[f], scale.inv * inv_back, sum);
+      for (int s = 0; s < 2; ++s) {
+        add_product(sum, fragment(back, (f * 2 + s) * 2), dg[s]);
+        add_product(sum, fragment(back, (f * 2 + s) * 2 + 1), du[s]);
+      }
+      add(dx[f], scale.inv, sum);
     }
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
 #pragma unroll
-  for (int f = 0; f < FT; ++f) store_tile(dx[f], out, (f0 + f) * kTile, a.F, a.vec_o, g);
+  for (int f = 0; f < FT; ++f) store_tile(unscaled(dx[f], a.inv_out + (f0 + f) * kTile, nullptr, g), out, (f0 + f) * kTile, a.F, a.vec_o, g);
 }
 
 template <int ACT, int FQ>

@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + 2 * OT <= 16 ? 2 : 1) k_ff_
   const float inv_x = load_row(x, a.X[at.t] + at.i * a.ldx, g, a.F, a.vec_x);
   f32x16 y[OT];
 #pragma unroll
-  for (int o = 0; o < OT; ++o) y[o] = per_row(a.bd + o * kTile, g);
+  for (int o = 0; o < OT; ++o) y[o] = zeros();
   for (int h = 0; h < a.ht; ++h) {
     staged();
     stage<WAVES, kDown>(a.down + (int64_t)h * kDown, down);
@@ -36,23 +36,26 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + 2 * OT <= 16 ? 2 : 1) k_ff_
       add_product(su, fragment(gu, 2 * q + 1), x[q]);
     }
     const TileVectors &v = vectors_of(gu, FQ);
-    const float inv = inv_x * v.inv_gu, inv_down = v.inv_down;
-    f32x16 G = value_of(sg, inv, v.bg, g);
-    const f32x16 U = value_of(su, inv, v.bu, g);
+    f32x16 G = value_of(sg, inv_x, v.inv_g, v.bg, g);
+    const f32x16 U = value_of(su, inv_x, v.inv_u, v.bu, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
     const Scale scale = scale_for(max_over_32(largest_of(G)));
-    const Split b[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)};
+    const Split b[2] = {half(G, 0, scale.to), half(G, 1, scale.to)};
     staged();
     if (h + 1 < a.ht) stage<WAVES, kGu>(a.gu + (int64_t)(h + 1) * kGu, gu);
 #pragma unroll
-    for (int o = 0; o < OT; ++o)
-      add(y[o], scale.inv * inv_down, product(fragment(down, 2 * o + 1), b[1], product(fragment(down, 2 * o), b[0], zeros())));
+    for (int o = 0; o < OT; ++o) {
+      Sums sum = no_sums();
+#pragma unroll
+      for (int s = 0; s < 2; ++s) add_product(sum, fragment(down, 2 * o + s), b[s]);
+      add(y[o], scale.inv, sum);
+    }
   }
   if (base + m >= a.rows) return;
   float *const out = a.out[at.t] + at.i * a.ldo;
 #pragma unroll
-  for (int o = 0; o < OT; ++o) store_tile(y[o], out, o * kTile, a.Fo, a.vec_o, g);
+  for (int o = 0; o < OT; ++o) store_tile(unscaled(y[o], a.inv_out + o * kTile, a.bd + o * kTile, g), out, o * kTile, a.Fo, a.vec_o, g);
 }
 
 template <int ACT, int FQ, int OT>

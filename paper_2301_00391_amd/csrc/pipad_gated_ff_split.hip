@@ -41,8 +41,9 @@ __device__ inline float share_rows(u32x4 *to, float (&largest)[kWaves][kTile], c
   return scale.inv;
 }
 
-// Columns c0 .. c0 + 31 of the rows: the waves' results added up, and a vector; the first four waves store 8 columns each.
-__device__ inline void store_sum(float (&part)[kWaves][16][kWave], const f32x16 &mine, const float *bias, float *row, bool there, int c0, int F, bool vec) {
+// Columns c0 .. c0 + 31 of the rows: the waves' results added up, times 1 over the columns' scales, and a vector; the first four waves store 8
+// columns each.
+__device__ inline void store_sum(float (&part)[kWaves][16][kWave], const f32x16 &mine, const float *inv, const float *bias, float *row, bool there, int c0, int F, bool vec) {
   const int lane = threadIdx.x & (kWave - 1), g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 #pragma unroll
   for (int r = 0; r < 16; ++r) part[wave][r][lane] = mine[r];
@@ -52,9 +53,10 @@ __device__ inline void store_sum(float (&part)[kWaves][16][kWave], const f32x16 
     float s[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      s[e] = bias ? bias[c + e] : 0.f;
+      s[e] = 0.f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) s[e] += part[w][4 * wave + e][lane];
+      s[e] = fmaf(s[e], inv[c + e], bias ? bias[c + e] : 0.f);
     }
     if (vec && c + 4 <= F) {
       *reinterpret_cast<float4 *>(row + c) = make_float4(s[0], s[1], s[2], s[3]);
@@ -89,20 +91,23 @@ __global__ void __launch_bounds__(kWaves *kWave, 2) k_ff_split(FfArgs a) {
       add_product(sg, fragment(gu, 2 * q), x);
       add_product(su, fragment(gu, 2 * q + 1), x);
     }
-    const float inv = inv_x * v.inv_gu;
-    f32x16 G = value_of(sg, inv, v.bg, g);
-    const f32x16 U = value_of(su, inv, v.bu, g);
+    f32x16 G = value_of(sg, inv_x, v.inv_g, v.bg, g);
+    const f32x16 U = value_of(su, inv_x, v.inv_u, v.bu, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) G[r] = activate<ACT>(G[r]) * U[r];
     const Scale scale = scale_for(max_over_32(largest_of(G)));
-    const Split b[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)};
+    const Split b[2] = {half(G, 0, scale.to), half(G, 1, scale.to)};
 #pragma unroll
-    for (int o = 0; o < OT; ++o)
-      add(y[o], scale.inv * v.inv_down, product(fragment(down, 2 * o + 1), b[1], product(fragment(down, 2 * o), b[0], zeros())));
+    for (int o = 0; o < OT; ++o) {
+      Sums sum = no_sums();
+#pragma unroll
+      for (int s = 0; s < 2; ++s) add_product(sum, fragment(down, 2 * o + s), b[s]);
+      add(y[o], scale.inv, sum);
+    }
   }
   float *const out = a.out[at.t] + at.i * a.ldo;
 #pragma unroll
-  for (int o = 0; o < OT; ++o) store_sum(part, y[o], a.bd, out, base + m < a.rows, o * kTile, a.Fo, a.vec_o);
+  for (int o = 0; o < OT; ++o) store_sum(part, y[o], a.inv_out, a.bd, out, base + m < a.rows, o * kTile, a.Fo, a.vec_o);
 }
 
 // FT tiles of X's columns from tile blockIdx.y * FT on.
@@ -131,12 +136,11 @@ __global__ void __launch_bounds__(kWaves *kWave, 2) k_ff_split_backward(FfArgs a
       add_product(sg, fragment(gu, 2 * q), x);
       add_product(su, fragment(gu, 2 * q + 1), x);
     }
-    const float inv = inv_x * v.inv_gu;
-    f32x16 G = value_of(sg, inv, v.bg, g), U = value_of(su, inv, v.bu, g);
+    f32x16 G = value_of(sg, inv_x, v.inv_g, v.bg, g), U = value_of(su, inv_x, v.inv_u, v.bu, g);
     Sums sd = no_sums();
 #pragma unroll 4
     for (int q = 0; q < a.oq; ++q) add_product(sd, fragment(up, q), fragment(dys, q));
-    const f32x16 dH = value_of(sd, inv_dy * v.inv_up);
+    const f32x16 dH = value_of(sd, inv_dy, v.inv_d, g);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float2 c = activate_slope<ACT>(G[r]);
@@ -144,18 +148,21 @@ __global__ void __launch_bounds__(kWaves *kWave, 2) k_ff_split_backward(FfArgs a
       U[r] = dH[r] * c.x;
     }
     const Scale scale = scale_for(max_over_32(largest_of(U, largest_of(G))));
-    const Split dg[2] = {half<false>(G, 0, scale.to), half<false>(G, 1, scale.to)}, du[2] = {half<false>(U, 0, scale.to), half<false>(U, 1, scale.to)};
+    const Split dg[2] = {half(G, 0, scale.to), half(G, 1, scale.to)}, du[2] = {half(U, 0, scale.to), half(U, 1, scale.to)};
 #pragma unroll
     for (int f = 0; f < FT; ++f) {
-      f32x16 sum = zeros();
+      Sums sum = no_sums();
 #pragma unroll
-      for (int s = 0; s < 2; ++s) sum = product(fragment(back, (f * 2 + s) * 2 + 1), du[s], product(fragment(back, (f * 2 + s) * 2), dg[s], sum));
-      add(dx[f], scale.inv * v.inv_back, sum);
+      for (int s = 0; s < 2; ++s) {
+        add_product(sum, fragment(back, (f * 2 + s) * 2), dg[s]);
+        add_product(sum, fragment(back, (f * 2 + s) * 2 + 1), du[s]);
+      }
+      add(dx[f], scale.inv, sum);
     }
   }
   float *const out = a.out[at.t] + at.i * a.ldo;
 #pragma unroll
-  for (int f = 0; f < FT; ++f) store_sum(part, dx[f], nullptr, out, base + m < a.rows, (f0 + f) * kTile, a.F, a.vec_o);
+  for (int f = 0; f < FT; ++f) store_sum(part, dx[f], a.inv_out, nullptr, out, base + m < a.rows, (f0 + f) * kTile, a.F, a.vec_o);
 }
 
 template <int ACT>
