@@ -16,11 +16,10 @@
 // A 16-bit float reaches from 2^-24 to 2^16, so operands are scaled, by powers of two: rows of X and dY by their largest value, weights by the
 // largest of the column that a result sees (Wg's and Wu's columns for G and U, Wd's rows for dH, Wd's columns for Y, and for dX the rows of Wg and
 // Wu, which share one), so that a huge or infinite weight is a matter of its own column; H, dG and dU by the largest of a node's (or in the weights'
-// gradients a hidden column's) 32 values at a time, whose products are added up outside.  Largest values come to 2^14 .. 2^15.  Two forms:
-//  - wide, forward and in the gradient of X: h2 is kept 2^11 larger and its products are summed apart, so that values down to 2^-29 of the
-//    largest have all their bits, and smaller ones an error of 2^-51 of it;
-//  - narrow, in the weights' gradients, which the additions to two sums bound: h2 as it is, one sum; all bits down to 2^-18 of the largest, an
-//    error of 2^-40 of it below.
+// gradients a hidden column's) 32 values at a time, whose products are added up outside.  Largest values come to 2^14 .. 2^15.  h2 is kept 2^11
+// larger and its products are summed apart, so that values down to 2^-29 of the largest have all their bits, and smaller ones an error of 2^-51 of
+// it.  With h2 as it is and one sum they have them down to 2^-18, and an error of 2^-40 below, which columns of X at 2^-20 of the others, or gates that
+// are nearly closed, come to: 6 % less time forward and 10 % backward (64 columns through 256) would not pay for that.
 // A value that is not finite makes its row NaN (or infinite).
 //
 // An instruction aligns what it adds to the largest of it and cuts off, so a sum comes out low by some 1e-8 of its terms' size; over millions of
@@ -45,7 +44,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32, kDepth = 16;
 constexpr int kFragment = 2 * kWave;  // the two pieces of a 32 x 16 operand, in 16-byte words
-constexpr float kWide = 2048.f;       // what h2 is multiplied by in the wide form
+constexpr float kWide = 2048.f;       // what h2 is multiplied by
 // Wg's and Wu's fragments of a hidden tile, and its vectors behind them (struct TileVectors).
 __host__ __device__ constexpr int gu_words(int fq) { return fq * 2 * kFragment + kWave; }
 struct TileVectors {
@@ -92,20 +91,16 @@ __device__ inline float max_of_wave(float x) {
 struct Split {
   u32x4 p[2];
 };
-template <bool WIDE>
 __device__ inline Split split8(const float (&v)[8], float scale) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
   typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-  constexpr float kBy = WIDE ? kWide : 1.f;
-  const float by = scale * kBy;
   Split s;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    // (as multiply-adds that take and give 16 bits, and in one register from there on: three and a half instructions a value)
-    uint32_t both = __builtin_bit_cast(uint32_t, (f16x2{(_Float16)fmaf(v[2 * i], scale, 0.f), (_Float16)fmaf(v[2 * i + 1], scale, 0.f)}));
-    asm("" : "+v"(both));
-    const f16x2 h = __builtin_bit_cast(f16x2, both);
-    const f16x2 rest{(_Float16)fmaf((float)h[0], -kBy, v[2 * i] * by), (_Float16)fmaf((float)h[1], -kBy, v[2 * i + 1] * by)};
-    s.p[0][i] = both;
+    const float a = v[2 * i] * scale, b = v[2 * i + 1] * scale;
+    const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
+    const f16x2 rest = __builtin_convertvector((f32x2{fmaf((float)h[0], -kWide, a * kWide), fmaf((float)h[1], -kWide, b * kWide)}), f16x2);
+    s.p[0][i] = __builtin_bit_cast(uint32_t, h);
     s.p[1][i] = __builtin_bit_cast(uint32_t, rest);
   }
   return s;
@@ -121,7 +116,7 @@ __device__ inline f32x16 zeros() {
 __device__ inline f32x16 mfma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-struct Sums {  // of wide products: main + cross / kWide
+struct Sums {  // main + cross / kWide
   f32x16 main, cross;
 };
 __device__ inline Sums no_sums() { return {zeros(), zeros()}; }
@@ -167,11 +162,11 @@ __device__ inline float largest_of(const f32x16 &x, float so_far = 0.f) {
   for (int r = 0; r < 16; ++r) so_far = max_of(so_far, x[r]);
   return so_far;
 }
-__device__ inline Split half(const f32x16 &r, int s, float scale) {  // the registers 8 s .. 8 s + 7 as a wide operand
+__device__ inline Split half(const f32x16 &r, int s, float scale) {  // the registers 8 s .. 8 s + 7 as an operand
   float v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = r[8 * s + j];
-  return split8<true>(v, scale);
+  return split8(v, scale);
 }
 
 // A sum of many terms that carries what the additions round off (over thousands of tiles a plain one is off by more than 1e-6).
@@ -235,7 +230,7 @@ struct FfArgs {
   int32_t n, k, F, hidden, Fo;
   int32_t ht, fq, oq, ft, ot;  // 32-column tiles of the hidden columns, 16- and 32-column tiles of X's and Y's
   bool vec_x, vec_dy, vec_o;
-  // Weights as fragments, all wide.  gu: [ht], each [fq][Wg, Wu], m = hidden column, depth = X's columns, and a TileVectors behind them.
+  // Weights as fragments.  gu: [ht], each [fq][Wg, Wu], m = hidden column, depth = X's columns, and a TileVectors behind them.
   // up: [ht][oq], m = hidden, depth = Y's columns (Wd).  down: [ht][ot][2], m = Y's column, depth of a result = hidden.
   // back: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
   const u32x4 *gu, *down, *up, *back;
@@ -272,7 +267,7 @@ __device__ inline void load8(float (&v)[8], const float *p, int c, int F, bool v
     }
   }
 }
-// A row of up to 16 N columns, whose other half lane m + 32 has, as wide pieces; returns 1 over its scale.
+// A row of up to 16 N columns, whose other half lane m + 32 has, as pieces; returns 1 over its scale.
 template <int N>
 __device__ inline float load_row(Split (&x)[N], const float *row, int g, int F, bool vec) {
   float v[N][8], largest = 0.f;
@@ -282,7 +277,7 @@ __device__ inline float load_row(Split (&x)[N], const float *row, int g, int F, 
   for (int q = 0; q < N; ++q) largest = largest_of(v[q], largest);
   const Scale s = scale_for(max_over_32(largest));
 #pragma unroll
-  for (int q = 0; q < N; ++q) x[q] = split8<true>(v[q], s.to);
+  for (int q = 0; q < N; ++q) x[q] = split8(v[q], s.to);
   return s.inv;
 }
 // A column vector, one value a row of a result.

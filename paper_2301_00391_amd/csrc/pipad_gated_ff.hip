@@ -94,11 +94,11 @@ __device__ inline void pack_hidden(const PackArgs &a, int h, float (&found)[2][k
         const int f = at / 2 * kDepth + 8 * g + j;
         v[j] = f < a.F && there ? W[f * ld + h0 + m] : 0.f;
       }
-      s = split8<true>(v, at % 2 ? scale_u.to : scale_g.to);
+      s = split8(v, at % 2 ? scale_u.to : scale_g.to);
       to = tile + at * kFragment;
     } else {  // [oq]
       load8(v, a.Wd + (there ? h0 + m : 0) * a.ldwd, (at - n_gu) * kDepth + 8 * g, there ? a.Fo : 0, false);
-      s = split8<true>(v, scale_d.to);
+      s = split8(v, scale_d.to);
       to = a.up + ((int64_t)h * n_up + at - n_gu) * kFragment;
     }
 #pragma unroll
@@ -124,7 +124,7 @@ __device__ inline void pack_down(const PackArgs &a, int o, int first, float (&fo
       const int hid = (first + at / 2) * kTile + result_depth(at % 2, g, j);
       v[j] = hid < a.hidden && there ? a.Wd[hid * a.ldwd + c] : 0.f;
     }
-    const Split s = split8<true>(v, scale.to);
+    const Split s = split8(v, scale.to);
     u32x4 *const to = a.down + (((int64_t)(first + at / 2) * a.ot + o) * 2 + at % 2) * kFragment;
 #pragma unroll
     for (int p = 0; p < 2; ++p) to[p * kWave + lane] = s.p[p];
@@ -148,7 +148,7 @@ __device__ inline void pack_back(const PackArgs &a, int t, int first, float (&ro
       const int hid = (first + at / 4) * kTile + result_depth(at / 2 % 2, g, j);
       v[j] = hid < a.hidden && f < a.F ? W[f * ld + hid] : 0.f;
     }
-    const Split s = split8<true>(v, scale.to);
+    const Split s = split8(v, scale.to);
     u32x4 *const to = a.back + (((int64_t)(first + at / 4) * a.ft + t) * 4 + at % 4) * kFragment;
 #pragma unroll
     for (int p = 0; p < 2; ++p) to[p * kWave + lane] = s.p[p];
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
       for (int q = 0; q < a.fq; ++q) {
         float v[8];
         load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
-        const Split b = split8<true>(v, scale_x.to);
+        const Split b = split8(v, scale_x.to);
         add_product(sg, fragment(gu, 2 * q), b);
         add_product(su, fragment(gu, 2 * q + 1), b);
       }
@@ -322,13 +322,13 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
       float v[8];
       for (int q = 0; q < a.fq; ++q) {
         load8(v, x, q * kDepth + 8 * g, a.F, a.vec_x);
-        const Split b = split8<true>(v, scale_x.to);
+        const Split b = split8(v, scale_x.to);
         add_product(sg, fragment(gu, 2 * q), b);
         add_product(su, fragment(gu, 2 * q + 1), b);
       }
       for (int q = 0; q < a.oq; ++q) {
         load8(v, dy, q * kDepth + 8 * g, a.Fo, a.vec_dy);
-        add_product(sd, fragment(a.up, (int64_t)h * a.oq + q), split8<true>(v, scale_dy.to));
+        add_product(sd, fragment(a.up, (int64_t)h * a.oq + q), split8(v, scale_dy.to));
       }
       f32x16 G = value_of(sg, scale_x.inv, vectors.inv_g, vectors.bg, g), U = value_of(su, scale_x.inv, vectors.inv_u, vectors.bu, g);
       const f32x16 dH = value_of(sd, scale_dy.inv, vectors.inv_d, g);
@@ -408,13 +408,13 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
       float v[8];
       for (int q = 0; q < a.fq; ++q) {
         load8(v, x, q * kDepth + 8 * g, there ? a.F : 0, a.vec_x);
-        const Split b = split8<true>(v, sign * scale_x.to);
+        const Split b = split8(v, sign * scale_x.to);
         add_product(sg, b, fragment(gu, 2 * q));
         add_product(su, b, fragment(gu, 2 * q + 1));
       }
       for (int q = 0; q < a.oq; ++q) {
         load8(v, dy, q * kDepth + 8 * g, there ? a.Fo : 0, a.vec_dy);
-        add_product(sd, split8<true>(v, sign * scale_dy.to), fragment(a.up, (int64_t)h * a.oq + q));
+        add_product(sd, split8(v, sign * scale_dy.to), fragment(a.up, (int64_t)h * a.oq + q));
       }
       float vg[16], vu[16], vh[16], tile_g = 0.f, tile_u = 0.f;
 #pragma unroll
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
         for (int s = 0; s < 2; ++s) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = from[8 * s + j];
-          lay(shared.piece[turn][wave], index + s, split8<true>(v, scale.to), lane);
+          lay(shared.piece[turn][wave], index + s, split8(v, scale.to), lane);
         }
         return sign * scale.inv;
       };
@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(kBlock, 1) k_ff_weights_backward(FfArgs a) {
           }
 #pragma unroll
           for (int j = 0; j < 8; ++j) scaled[j] = v[j] * to[result_depth(s, g, j)];
-          return split8<true>(scaled, 1.f);
+          return split8(scaled, 1.f);
         };
         if (t0 + t < a.ft) {
           Sums g_sum = no_sums(), u_sum = no_sums();

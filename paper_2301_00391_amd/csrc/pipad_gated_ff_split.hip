@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kWaves = 8, kMostDepth = 16;  // tiles of 16 columns that a row has at most
 
-// Rows base .. base + 31 as wide pieces; returns 1 over the scale of the lane's row.  The waves have a tile of 16 columns each, of more than 8
+// Rows base .. base + 31 as pieces; returns 1 over the scale of the lane's row.  The waves have a tile of 16 columns each, of more than 8
 // tiles two.
 __device__ inline float share_rows(u32x4 *to, float (&largest)[kWaves][kTile], const float *row, int tiles_, int F, bool vec) {
   const int lane = threadIdx.x & (kWave - 1), m = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -34,7 +34,7 @@ __device__ inline float share_rows(u32x4 *to, float (&largest)[kWaves][kTile], c
   for (int s = 0; s < 2; ++s) {
     const int q = wave + s * kWaves;
     if (q < tiles_) {
-      const Split p = split8<true>(v[s], scale.to);
+      const Split p = split8(v[s], scale.to);
       to[q * kFragment + lane] = p.p[0], to[q * kFragment + kWave + lane] = p.p[1];
     }
   }

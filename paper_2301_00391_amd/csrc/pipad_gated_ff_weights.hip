@@ -32,11 +32,16 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 __device__ inline f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-__device__ inline f32x4 product16(const Split &a, const Split &b, f32x4 c) {  // as product()
-  c = mfma16(a.p[1], b.p[0], c);
-  c = mfma16(a.p[0], b.p[1], c);
-  return mfma16(a.p[0], b.p[0], c);
+struct Sums16 {  // as Sums
+  f32x4 main, cross;
+};
+__device__ inline Sums16 no_sums16() { return {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}; }
+__device__ inline void add_product16(Sums16 &c, const Split &a, const Split &b) {
+  c.cross = mfma16(a.p[1], b.p[0], c.cross);
+  c.main = mfma16(a.p[0], b.p[0], c.main);
+  c.cross = mfma16(a.p[0], b.p[1], c.cross);
 }
+__device__ inline float sum_of(const Sums16 &c, int r) { return fmaf(c.cross[r], 1.f / kWide, c.main[r]); }
 
 // The pieces of 32 rows of 32 D columns, two planes, and 1 over the rows' scales.  The 16-byte chunks of a row are permuted by its number, so that
 // 16 lanes that read a chunk of a row each, and 32 that read 8 bytes of eight rows, meet all 64 banks once: rows of 64 D bytes are 4 / D to the
@@ -88,7 +93,11 @@ template <int D, int AT, int THREADS>
 struct Share {
   static constexpr int kChunks = 4 * D, kUnits = kTile * kChunks, kMine = kUnits > THREADS ? kUnits / THREADS : 1;
   float v[kMine][8];
-  __device__ static int me() { return (int)threadIdx.x - AT; }
+  __device__ static int me() {
+    int at = (int)threadIdx.x - AT;
+    if (D > 4) asm("" : "+v"(at));  // (of 256 columns: what follows from it is made again each time, for the registers)
+    return at;
+  }
   __device__ static bool there() { return AT + kUnits >= THREADS ? AT == 0 || me() >= 0 : me() >= 0 && me() < kUnits; }
   __device__ static int row(int q) { return (q * THREADS + me()) / kChunks; }
   __device__ static int chunk() { return me() % kChunks; }
@@ -122,7 +131,7 @@ struct Share {
       if (kChunks >= 16) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));  // row_mirror: the other eight
       if (kChunks >= 32) x = __float_as_uint(max_over_16(__uint_as_float(x)));
       const Scale scale = scale_for(__uint_as_float(x));
-      slot.put(row(q), chunk(), split8<false>(v[q], sign * scale.to));
+      slot.put(row(q), chunk(), split8(v[q], sign * scale.to));
       if (chunk() == 0) slot.inv[row(q)] = scale.inv;
     }
   }
@@ -131,7 +140,7 @@ struct Share {
 // A lane's 8 values, a hidden column in four lanes, as pieces; returns 1 over their scale.
 __device__ inline float pieces_of(const float (&v)[8], Split *to) {
   const Scale scale = scale_for(max_over_32(max_over_16(largest_of(v))));
-  *to = split8<false>(v, scale.to);
+  *to = split8(v, scale.to);
   return scale.inv;
 }
 
@@ -150,27 +159,25 @@ __global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_
   const bool there = hid < a.hidden;
 
   Split wg[FD], wu[FD], wd[OD];
-  float inv_gu, inv_up;
-  {
-    float v[2][FD][8], largest = 0.f;
+  float inv_g, inv_u, inv_d;  // 1 over the scales of the lane's column of Wg and Wu and row of Wd, which four lanes share
+  const auto columns_of = [&](const float *W, int64_t ld, Split (&to)[FD], float *inv) {
+    float v[FD][8], largest = 0.f;
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
+    for (int q = 0; q < FD; ++q) {
 #pragma unroll
-      for (int q = 0; q < FD; ++q) {
-        const float *const W = w ? a.Wu : a.Wg;
-        const int64_t ld = w ? a.ldwu : a.ldwg;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int f = 32 * q + 8 * g + j;
-          v[w][q][j] = there && f < a.F ? W[f * ld + hid] : 0.f;
-        }
-        largest = largest_of(v[w][q], largest);
+      for (int j = 0; j < 8; ++j) {
+        const int f = 32 * q + 8 * g + j;
+        v[q][j] = there && f < a.F ? W[f * ld + hid] : 0.f;
       }
-    const Scale scale = scale_for(max_of_wave(largest));
-    inv_gu = scale.inv;
+      largest = largest_of(v[q], largest);
+    }
+    const Scale scale = scale_for(max_over_32(max_over_16(largest)));
+    *inv = scale.inv;
 #pragma unroll
-    for (int q = 0; q < FD; ++q) wg[q] = split8<false>(v[0][q], scale.to), wu[q] = split8<false>(v[1][q], scale.to);
-  }
+    for (int q = 0; q < FD; ++q) to[q] = split8(v[q], scale.to);
+  };
+  columns_of(a.Wg, a.ldwg, wg, &inv_g);
+  columns_of(a.Wu, a.ldwu, wu, &inv_u);
   {
     float v[OD][8], largest = 0.f;
 #pragma unroll
@@ -178,10 +185,10 @@ __global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_
       load8(v[q], a.Wd + (there ? hid : 0) * a.ldwd, 32 * q + 8 * g, there ? a.Fo : 0, false);
       largest = largest_of(v[q], largest);
     }
-    const Scale scale = scale_for(max_of_wave(largest));
-    inv_up = scale.inv;
+    const Scale scale = scale_for(max_over_32(max_over_16(largest)));
+    inv_d = scale.inv;
 #pragma unroll
-    for (int q = 0; q < OD; ++q) wd[q] = split8<false>(v[q], scale.to);
+    for (int q = 0; q < OD; ++q) wd[q] = split8(v[q], scale.to);
   }
   const float bg = there && a.bg ? a.bg[hid] : 0.f, bu = there && a.bu ? a.bu[hid] : 0.f;
   f32x4 dwg[2 * FS], dwu[2 * FS], dwd[2 * OS];  // dwd transposed: its rows are Y's columns
@@ -222,24 +229,25 @@ __global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_
   lay_down(0, 1.f);
   load_next();
   __syncthreads();
-  const f32x4 zero{0.f, 0.f, 0.f, 0.f};
   float sign = 1.f;
   for (int64_t i = 0; i < count; ++i) {
     const Slot<FD> &X = xs[i & 1];
     const Slot<OD> &dY = dys[i & 1];
-    f32x4 sg[2] = {zero, zero}, su[2] = {zero, zero}, sd[2] = {zero, zero};
+    int at = lane;
+    if (FD + OD > 12) asm("" : "+v"(at));  // (where there are not the registers to keep what follows from the lane: places in LDS)
+    Sums16 sg[2] = {no_sums16(), no_sums16()}, su[2] = {no_sums16(), no_sums16()}, sd[2] = {no_sums16(), no_sums16()};
     // an operand's loads are on the way while the one before is multiplied (one wave a SIMD waits for each of them otherwise)
     constexpr int kPlain = 2 * (FD + OD);
-    const auto plain = [&](int p) { return p < 2 * FD ? X.plain(p % 2, p / 2, lane) : dY.plain(p % 2, (p - 2 * FD) / 2, lane); };
+    const auto plain = [&](int p) { return p < 2 * FD ? X.plain(p % 2, p / 2, at) : dY.plain(p % 2, (p - 2 * FD) / 2, at); };
     Split now = plain(0);
 #pragma unroll
     for (int p = 0; p < kPlain; ++p) {
       const Split next = plain(p + 1 < kPlain ? p + 1 : 0);
       if (p < 2 * FD) {
-        sg[p % 2] = product16(now, wg[p / 2], sg[p % 2]);
-        su[p % 2] = product16(now, wu[p / 2], su[p % 2]);
+        add_product16(sg[p % 2], now, wg[p / 2]);
+        add_product16(su[p % 2], now, wu[p / 2]);
       } else {
-        sd[p % 2] = product16(now, wd[(p - 2 * FD) / 2], sd[p % 2]);
+        add_product16(sd[p % 2], now, wd[(p - 2 * FD) / 2]);
       }
       now = next;
       __builtin_amdgcn_sched_barrier(0);
@@ -249,7 +257,7 @@ __global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_
       load_next();
     }
     // X and dY have this tile's sign
-    const float sign_gu = sign * inv_gu, sign_up = sign * inv_up;
+    const float sign_g = sign * inv_g, sign_u = sign * inv_u, sign_d = sign * inv_d;
     float vg[8], vu[8], vh[8], tile_g = 0.f, tile_u = 0.f;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -257,9 +265,8 @@ __global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int j = 4 * s + r;
-        const float cx = sign_gu * inv_x[r];
-        const float2 c = activate_slope<ACT>(fmaf(sg[s][r], cx, bg));
-        const float u = fmaf(su[s][r], cx, bu), d = sd[s][r] * (sign_up * inv_dy[r]);
+        const float2 c = activate_slope<ACT>(fmaf(sum_of(sg[s], r), sign_g * inv_x[r], bg));
+        const float u = fmaf(sum_of(su[s], r), sign_u * inv_x[r], bu), d = sum_of(sd[s], r) * (sign_d * inv_dy[r]);
         vg[j] = d * u * c.y;
         vu[j] = d * c.x;
         tile_g += vg[j];
@@ -272,14 +279,14 @@ __global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_
     dbg.add(tile_g), dbu.add(tile_u);
     Split dg, du, hh;
     const float cg = sign * pieces_of(vg, &dg), cu = sign * pieces_of(vu, &du), ch = sign * pieces_of(vh, &hh);
-    const auto add = [](f32x4 &to, float factor, const f32x4 &x) {
+    const auto add = [](f32x4 &to, float factor, const Sums16 &x) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[r] = fmaf(x[r], factor, to[r]);
+      for (int r = 0; r < 4; ++r) to[r] = fmaf(sum_of(x, r), factor, to[r]);
     };
     // likewise, and a product's sums are added while the next one is made
     constexpr int kTransposed = 2 * (FS + OS);
-    const auto transposed = [&](int p) { return p < 2 * FS ? X.transposed(2 * f0 + p, lane) : dY.transposed(2 * o0 + p - 2 * FS, lane); };
-    f32x4 sums[2];
+    const auto transposed = [&](int p) { return p < 2 * FS ? X.transposed(2 * f0 + p, at) : dY.transposed(2 * o0 + p - 2 * FS, at); };
+    Sums16 sums[2];
     const auto add_sums = [&](int p) {
       if (p < 2 * FS) {
         add(dwg[p], cg, sums[0]);
@@ -292,10 +299,11 @@ __global__ void __launch_bounds__(WAVES *kWave, FD + OD <= 4 ? 2 : 1) k_ff_kept_
 #pragma unroll
     for (int p = 0; p < kTransposed; ++p) {
       const Split next = transposed(p + 1 < kTransposed ? p + 1 : 0);
-      const f32x4 first = product16(now, p < 2 * FS ? dg : hh, zero);
-      const f32x4 second = p < 2 * FS ? product16(now, du, zero) : zero;
+      Sums16 made[2] = {no_sums16(), no_sums16()};
+      add_product16(made[0], now, p < 2 * FS ? dg : hh);
+      if (p < 2 * FS) add_product16(made[1], now, du);
       if (p > 0) add_sums(p - 1);
-      sums[0] = first, sums[1] = second;
+      sums[0] = made[0], sums[1] = made[1];
       now = next;
       __builtin_amdgcn_sched_barrier(0);
     }

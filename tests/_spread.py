@@ -26,8 +26,3 @@ def columns_off(got, want, dim):
 def check_columns(got, want, dim, limit, what):
     off = columns_off(got, want, dim)
     assert bool((off <= limit).all()), f"{what}: {int((~(off <= limit)).sum())} of {off.numel()} beyond {limit:.1e}, worst {float(off.nan_to_num(nan=1e30).max()):.3g}"
-
-
-#: which way a result's columns lie that see one column of an operand each: dX's columns belong to X's, dWg's rows to X's columns and its columns to
-#: hidden columns, dWd's rows to hidden columns and its columns to Y's
-GRADIENTS = {"dX": (0,), "dWg": (0, 1), "dWu": (0, 1), "dWd": (0, 1)}
