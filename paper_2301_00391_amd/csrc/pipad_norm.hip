@@ -212,13 +212,37 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
   __shared__ float sums[2][kWavesPerBlock][LPR < 256 ? E * LPR : 1];  // (more than one row a workgroup; in turns: one barrier a sum)
   int turn = 0;
   const int lane = threadIdx.x % LPR, t = blockIdx.y, F = a.F;
-  R scale, w_post, b_post, w_pre, acc[kSums];
+  R scale, w_post, b_post, w_pre, acc[kSums], rest[kSums];
   scale.load_or(a.scale, lane, F, 1.f);
   w_post.load_or(a.w_post, lane, F, 1.f);
   b_post.load_or(a.b_post, lane, F, 0.f);
   w_pre.load_or(a.w_pre, lane, F, 1.f);
 #pragma unroll
-  for (int q = 0; q < kSums; ++q) acc[q].fill(0.f);
+  for (int q = 0; q < kSums; ++q) acc[q].fill(0.f), rest[q].fill(0.f);
+  // A plain chain of additions would be off by more the more rows a lane has (4 million rows of 128: 3.5e-7 of the sums' size, so 1.0e-7).  A sum of few
+  // columns a lane carries what its additions round off, in `rest`, at no cost; of more columns, whose registers are short, 64 rows are added up by
+  // themselves and then to `rest` (256 MB a matrix, as plain chains, so, and carried: 512 columns 398, 420 and 422 us, 1022 columns 612, 621 and 663,
+  // 4096 columns 632, 595 and 636, 4094 columns 687, 760 and 813).
+  constexpr bool kCarry = E <= 4;
+  constexpr int kChain = 64;
+  int chain = 0;
+  const auto add = [&](int q, int j, float x, float y) {
+    float &sum = acc[q].v[j], &lost = rest[q].v[j];
+    if (!kCarry) {
+      sum = fmaf(x, y, sum);
+      return;
+    }
+    const float z = fmaf(x, y, -lost), s = sum + z;
+    lost = (s - sum) - z;
+    sum = s;
+  };
+  const auto end_chain = [&] {
+#pragma unroll
+    for (int q = 0; q < kSums; ++q)
+#pragma unroll
+      for (int j = 0; j < E; ++j) rest[q].v[j] += acc[q].v[j], acc[q].v[j] = 0.f;
+    chain = 0;
+  };
   struct Loaded {
     R b, gate, g, x, d;
   };
@@ -244,8 +268,8 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
       const float r = normalise(x, a.pre, lane, F, a.inv_f, a.eps, lds, turn);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        acc[3].v[j] = fmaf(d.v[j], x.v[j], acc[3].v[j]);
-        acc[4].v[j] += d.v[j];
+        add(3, j, d.v[j], x.v[j]);
+        add(4, j, d.v[j], 1.f);
         d.v[j] *= w_pre.v[j];
       }
       normalise_back(d, x, r, a.pre, a.inv_f, lds, turn);
@@ -264,11 +288,11 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
           // (1 - sigmoid) from the same exponential: their difference would lose it where the gate is wide open
           const float e = __expf(-fabsf(gate.v[j])), big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
           const float sig = gate.v[j] >= 0.f ? big : small;
-          acc[0].v[j] = fmaf(g.v[j], sig * p, acc[0].v[j]);
+          add(0, j, g.v[j], sig * p);
           gate.v[j] = gs * p * big * small;
           gs *= sig;
         } else {
-          acc[0].v[j] = fmaf(g.v[j], p, acc[0].v[j]);
+          add(0, j, g.v[j], p);
         }
         d.v[j] = gs;
       }
@@ -276,31 +300,34 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
       if (a.post != PIPAD_NORM_NONE) {
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-          acc[1].v[j] = fmaf(d.v[j], b.v[j], acc[1].v[j]);
-          acc[2].v[j] += d.v[j];
+          add(1, j, d.v[j], b.v[j]);
+          add(2, j, d.v[j], 1.f);
           d.v[j] = d.column(lane, j) < F ? d.v[j] * w_post.v[j] : 0.f;
         }
         normalise_back(d, b, r, a.post, a.inv_f, lds, turn);
       }
       if (a.want1) d.store(a.out1[t] + i * a.ld1, lane, F);
     }
+    if (!kCarry && ++chain == kChain) end_chain();
   }
   if (!a.partial) return;
+  if (!kCarry) end_chain();
+  const R *const total = kCarry ? acc : rest;
   float *const to = a.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kSums * F;
 #pragma unroll
   for (int q = 0; q < kSums; ++q) {
     if (LPR == 256) {
 #pragma unroll
       for (int j = 0; j < E; ++j)
-        if (acc[q].column(lane, j) < F) to[q * F + acc[q].column(lane, j)] = acc[q].v[j];
+        if (total[q].column(lane, j) < F) to[q * F + total[q].column(lane, j)] = total[q].v[j];
       continue;
     }
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      float x = acc[q].v[j];
+      float x = total[q].v[j];
 #pragma unroll
       for (int d = LPR; d < kWave; d *= 2) x += __shfl_xor(x, d);
-      if (threadIdx.x % kWave < LPR) sums[q & 1][threadIdx.x / kWave][acc[q].column(lane, j)] = x;
+      if (threadIdx.x % kWave < LPR) sums[q & 1][threadIdx.x / kWave][total[q].column(lane, j)] = x;
     }
     __syncthreads();
     const auto &of = sums[q & 1];
