@@ -234,7 +234,7 @@ struct FfArgs {
   // up: [ht][oq], m = hidden, depth = Y's columns (Wd).  down: [ht][ot][2], m = Y's column, depth of a result = hidden.
   // back: [ht][ft][2][Wg, Wu], m = X's column, depth of a result = hidden.
   const u32x4 *gu, *down, *up, *back;
-  const float *inv_out, *bd;  // 1 over the scales of down's or back's columns, and bd; padded to whole tiles
+  const float *inv_out, *bd;  // 1 over the scales of down's or back's columns, over kToOne, and bd; padded to whole tiles
   const float *Wg, *Wu, *Wd, *bg, *bu, *bd_in;  // as they came
   int64_t ldwg, ldwu, ldwd;
   // weight gradients: partial sums of `parts` ranges of rows, each [dWg F x hidden | dWu | dWd hidden x Fo | dbg | dbu | dbd]
@@ -290,6 +290,9 @@ __device__ inline f32x16 per_row(const float *p, int g) {
   }
   return z;
 }
+// Sums of Y's and dX's columns are kept for weights that come to 1 .. 2, not to 2^14 .. 2^15: they are about as large as H's, or dG's and dU's, sums then,
+// and end where those do.
+constexpr float kToOne = 1.f / 16384.f;
 // Y's or dX's columns c0 .. as they are: times 1 over their scales, and Y's bias.
 __device__ inline f32x16 unscaled(const f32x16 &sums, const float *inv, const float *bias, int g) {
   f32x16 z = per_row(inv, g), b = zeros();

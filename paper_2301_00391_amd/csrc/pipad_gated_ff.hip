@@ -115,7 +115,7 @@ __device__ inline void pack_down(const PackArgs &a, int o, int first, float (&fo
   if (g == 0) found[wave][m] = largest[0];
   __syncthreads();
   const Scale scale = scale_of(found, m);
-  if (first == 0 && threadIdx.x < kTile) a.inv_out[c] = scale.inv, a.pbd[c] = a.bd && there ? a.bd[c] : 0.f;
+  if (first == 0 && threadIdx.x < kTile) a.inv_out[c] = scale.inv / kToOne, a.pbd[c] = a.bd && there ? a.bd[c] : 0.f;
   const int count = 2 * min(a.ht - first, a.tiles);
   for (int at = wave; at < count; at += kPackWaves) {  // [2]
     float v[8];
@@ -137,7 +137,7 @@ __device__ inline void pack_back(const PackArgs &a, int t, int first, float (&ro
   largest_of_rows<2>(rows, {a.Wg, a.Wu}, {a.ldwg, a.ldwu}, t * kTile, a.F, a.hidden, lane, wave);
   __syncthreads();
   const Scale scale = scale_for(rows[m]);
-  if (first == 0 && threadIdx.x < kTile) a.inv_out[f] = scale.inv;
+  if (first == 0 && threadIdx.x < kTile) a.inv_out[f] = scale.inv / kToOne;
   const int count = 4 * min(a.ht - first, a.tiles);
   for (int at = wave; at < count; at += kPackWaves) {  // [2][Wg, Wu]
     const float *W = at % 2 ? a.Wu : a.Wg;
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
       const Scale scale = scale_for(max_over_32(largest_of(G)));
 #pragma unroll
       for (int s = 0; s < 2; ++s) lay(hs.piece[turn][wave], s, half(G, s, scale.to), lane);
-      hs.inv[turn][wave][lane] = scale.inv;
+      hs.inv[turn][wave][lane] = scale.inv * kToOne;
     }
     __syncthreads();
     const int count = min(a.ht - h0, kWavesPerBlock);
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows_backward(FfArgs a) {
         lay(ds.piece[turn][wave], s, half(G, s, scale.to), lane);
         lay(ds.piece[turn][wave], 2 + s, half(U, s, scale.to), lane);
       }
-      ds.inv[turn][wave][lane] = scale.inv;
+      ds.inv[turn][wave][lane] = scale.inv * kToOne;
     }
     __syncthreads();
     const int count = min(a.ht - h0, kWavesPerBlock);

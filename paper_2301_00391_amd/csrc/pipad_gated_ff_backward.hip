@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + OQ <= 8 ? 2 : 1) k_ff_kept_
         add_product(sum, fragment(back, (f * 2 + s) * 2), dg[s]);
         add_product(sum, fragment(back, (f * 2 + s) * 2 + 1), du[s]);
       }
-      add(dx[f], scale.inv, sum);
+      add(dx[f], scale.inv * kToOne, sum);
     }
   }
   if (base + m >= a.rows) return;

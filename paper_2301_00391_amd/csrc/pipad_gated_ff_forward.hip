@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(WAVES *kWave, FQ + 2 * OT <= 16 ? 2 : 1) k_ff_
       Sums sum = no_sums();
 #pragma unroll
       for (int s = 0; s < 2; ++s) add_product(sum, fragment(down, 2 * o + s), b[s]);
-      add(y[o], scale.inv, sum);
+      add(y[o], scale.inv * kToOne, sum);
     }
   }
   if (base + m >= a.rows) return;

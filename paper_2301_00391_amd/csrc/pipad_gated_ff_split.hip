@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kWaves *kWave, 2) k_ff_split(FfArgs a) {
       Sums sum = no_sums();
 #pragma unroll
       for (int s = 0; s < 2; ++s) add_product(sum, fragment(down, 2 * o + s), b[s]);
-      add(y[o], scale.inv, sum);
+      add(y[o], scale.inv * kToOne, sum);
     }
   }
   float *const out = a.out[at.t] + at.i * a.ldo;
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kWaves *kWave, 2) k_ff_split_backward(FfArgs a
         add_product(sum, fragment(back, (f * 2 + s) * 2), dg[s]);
         add_product(sum, fragment(back, (f * 2 + s) * 2 + 1), du[s]);
       }
-      add(dx[f], scale.inv, sum);
+      add(dx[f], scale.inv * kToOne, sum);
     }
   }
   float *const out = a.out[at.t] + at.i * a.ldo;

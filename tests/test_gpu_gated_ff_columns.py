@@ -114,3 +114,18 @@ def test_every_kernel_keeps_the_bits(pipad, rows, F, hidden, Fo):  # noqa: F811
         if activation != "relu":  # (whose slope jumps where G changes sign)
             dx = pipad.gated_ff_backward([X], [dY], *W, *b[:2], activation=activation, weights=False, biases=False).dX[0]
             check_columns(dx, want.backward(dY)["dX"][0], 0, LIMIT_GRADIENT, "dX")
+
+
+@pytest.mark.parametrize("rows,F,hidden,Fo", KERNELS)
+def test_large_hidden_values_and_small_weights(pipad, rows, F, hidden, Fo):  # noqa: F811
+    """H of 1e35 and more, where floats end at 3e38, and weights that bring Y and dX back: what lies between has to stay inside, too."""
+    _, (Wg, Wu, Wd), _, X, dY = case(rows, F, hidden, Fo)
+    Wg, Wu, Wd = Wg * 1e18, Wu * 1e17, Wd * 1e-30
+    want = GatedFF(X, Wg, Wu, Wd, None, None, None, "relu")
+    check_columns(pipad.gated_ff([X], Wg, Wu, Wd, activation="relu")[0], want.forward()[0], 0, LIMIT["Y"], "Y")
+    Wg, Wu, Wd = Wg * 1e-48, Wu * 1e-17, Wd * 1e30  # dU of 1e35, dG of 1e35, of weights of 1e-30
+    Wu = Wu * 1e-30
+    dy = dY * 1e35
+    bg, bu = torch.ones(hidden, device="cuda"), torch.ones(hidden, device="cuda")
+    want = GatedFF(X, Wg, Wu, Wd, bg, bu, None, "silu").backward(dy)["dX"][0]
+    check_columns(pipad.gated_ff_backward([X], [dy], Wg, Wu, Wd, bg, bu, weights=False, biases=False).dX[0], want, 0, LIMIT_GRADIENT, "dX")
