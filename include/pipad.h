@@ -339,10 +339,18 @@ int pipad_residual_norm_backward(const pipad_residual_norm_t *norm, int32_t n, i
  *   activation  sigmoid, relu, gelu (the exact one, x * Phi(x)) or silu (x * sigmoid(x))
  *   Wg, Wu      row-major float [F][hidden], row strides ldwg, ldwu >= hidden;  Wd  [hidden][Fo], ldwd >= Fo
  *   bg, bu, bd  float [hidden], [hidden], [Fo], NULL: none
- * Widths of 65536 and more, and more than 2^30 rows in all (2^28 of more than 256 columns), are PIPAD_ERR_TOO_LARGE.  Products are those of 32-bit floats to about their last
- * bits, from 16-bit pieces with scales (csrc/pipad_gated_ff.h): a row's values, and the weights of 32 hidden columns, are held to 2^-22 of
- * themselves, small ones to 2^-51 of the row's (block's) largest, in the weights' gradients to 2^-40 of it.  A row with a value that is not
- * finite gives NaN where floats may give an infinity, and no other row sees it.
+ * Widths of 65536 and more, and more than 2^30 rows in all (2^28 of more than 256 columns), are PIPAD_ERR_TOO_LARGE.
+ * Products are those of 32-bit floats to about their last bits: forward up to 256 rows (512 of more than 256 columns) in 32-bit arithmetic, else from
+ * two 16-bit pieces with scales (csrc/pipad_gated_ff.h).  An operand is held to 2^-22 of itself (2^-24 on average), and where it is less than 2^-29 of
+ * the largest that it shares a scale with, to 2^-51 of that one.  A scale is shared by
+ *  - a row of X, a row of dY;
+ *  - of the weights what goes into one column of a result: a column of Wg, one of Wu (G, U), a row of Wd (dH), a column of Wd (Y), the same row of
+ *    Wg and Wu (dX): a huge or infinite weight does not touch the others' columns, as it does not where floats are multiplied;
+ *  - 32 values of H, or of dG and dU together, of a row; in the weights' gradients the 32 rows' values of a hidden column in dG, dU or H, each times the
+ *    largest of its row of X, or dY.
+ * So beside floats bits are lost where a sum's terms are products of large and very small values (a column of X at 2^-40 of the others whose weights are
+ * 2^40 of theirs).  A row with a value that is not finite gives NaN where floats may give an infinity, and no other row sees it; a weight that is not
+ * finite does so in the results that it is a factor of.
  *  Made for rows of up to 256 columns: for many wider ones the weights' gradients take several times what single matrix products would. */
 #define PIPAD_ACT_SIGMOID 0
 #define PIPAD_ACT_RELU 1
@@ -369,7 +377,7 @@ typedef struct pipad_gated_ff_grads {
 
 /* The gradients of pipad_gated_ff from X and dY: nothing is kept from the forward call, what lies between is made again.
  *   dX      receives the gradient of X; NULL: not wanted
- *   grads   NULL: none wanted */
+ *   grads   NULL: none wanted.  Any of them alone takes as long as all */
 int pipad_gated_ff_backward(const pipad_gated_ff_t *block, int32_t n, int32_t k, const float *const *X, int64_t ldx,
                             const float *const *dY, int64_t lddy, float *const *dX, int64_t lddx,
                             const pipad_gated_ff_grads_t *grads, void *workspace, size_t workspace_bytes, void *stream);

@@ -10,8 +10,8 @@
 // h1 k2 + h2 k1, the fourth product being below 2^-22 of the whole, summed in 32 bits.  Pieces hold 22 bits and a sign, so an operand is off by
 // 2^-22 at most and 2^-24 on average; the error of a sum of 64 products came out as 1.0e-7 of its size (1.4e-7 for a chain of 32-bit
 // multiply-adds, whose roundings are more).  Three instructions of 32 cycles for 32 x 32 x 16 are 5.3 times as fast as the matrix instructions on
-// floats; bf16 pieces hold the last two bits, too, but take three each and six products, and the card's power is what bounds these
-// kernels: 8 million rows of 64 through 171 columns took 2.85 ms with them and take 2.08 now.
+// floats; bf16 pieces hold the last two bits, too, and reach as far as floats do, but take three each and six products, and issue and the card's
+// power are what bounds these kernels: 8 million rows of 64 through 171 columns took 2.85 ms with them and take 2.21 now.
 //
 // A 16-bit float reaches from 2^-24 to 2^16, so operands are scaled, by powers of two: rows of X and dY by their largest value, weights by the
 // largest of the column that a result sees (Wg's and Wu's columns for G and U, Wd's rows for dH, Wd's columns for Y, and for dX the rows of Wg and
@@ -19,7 +19,7 @@
 // gradients a hidden column's) 32 values at a time, whose products are added up outside.  Largest values come to 2^14 .. 2^15.  h2 is kept 2^11
 // larger and its products are summed apart, so that values down to 2^-29 of the largest have all their bits, and smaller ones an error of 2^-51 of
 // it.  With h2 as it is and one sum they have them down to 2^-18, and an error of 2^-40 below, which columns of X at 2^-20 of the others, or gates that
-// are nearly closed, come to: 6 % less time forward and 10 % backward (64 columns through 256) would not pay for that.
+// are nearly closed, come to: 7 % less time forward and 10 % backward (64 columns through 256) do not pay for that.
 // A value that is not finite makes its row NaN (or infinite).
 //
 // An instruction aligns what it adds to the largest of it and cuts off, so a sum comes out low by some 1e-8 of its terms' size; over millions of
@@ -182,8 +182,9 @@ struct Total {
 
 // ---- the activations ----------------------------------------------------------------------------
 // The normal distribution's tail Q(|x|) = 1 - Phi(|x|), and its density times sqrt(2 pi), exp(-x^2 / 2).  Q is that times a function that falls like
-// 1 / |x|: a polynomial in k = 1 / (1 + 0.275 |x|) without a constant term, fitted for the least error of |x| Q (1.1e-8, 6.9e-8 with the
-// arithmetic's own; of Q itself 4e-5 of it at most up to |x| = 4).  x Phi(x) = max(x, 0) - |x| Q(|x|) for either sign.
+// 1 / |x|: a polynomial in k = 1 / (1 + 0.275 |x|) without a constant term, which is the form of formula 26.2.17 in Abramowitz and Stegun's handbook,
+// fitted here for the least error of |x| Q (1.1e-8, 6.9e-8 with the arithmetic's own; of Q itself 4e-5 of it at most up to |x| = 4).
+// x Phi(x) = max(x, 0) - |x| Q(|x|) for either sign.
 struct Normal {
   float tail, density;
 };

@@ -1,9 +1,9 @@
 // The gated feed-forward block: weights as fragments, the kernels for rows of any width, and the host side.  How the products are
 // made stands in pipad_gated_ff.h; rows of up to 256 columns have kernels of their own in pipad_gated_ff_forward.hip, _backward.hip, _weights.hip
 // and, for few rows, _split.hip.  The kernels here for wider ones hold no row, but read it again for every hidden tile, and the waves of a workgroup make
-// a tile of H (dG and dU) each for all of them; of more than 512 columns another workgroup makes them again.  65536 rows of 512 through 2048: 3.0 ms
-// forward and 4.7 the gradient of X, where three and five products of float matrices take 2.7 and 4.5 and write H in between (each wave by itself:
-// 10.8 and 18.2); 29 the gradients of the weights (78), where six take 5.4: a column of X is loaded and split again for every hidden tile.
+// a tile of H (dG and dU) each for all of them; of more than 512 columns another workgroup makes them again.  65536 rows of 512 through 2048: 2.4 ms
+// forward and 3.9 the gradient of X, where three and five products of float matrices take 2.7 and 4.5 and write H in between; 29 the gradients of the
+// weights, where six take 5.4: a column of X is loaded and split again for every hidden tile.
 #include "pipad_gated_ff.h"
 
 namespace pipad {
@@ -242,8 +242,8 @@ __global__ void __launch_bounds__(kBlock, 2) k_ff_rows(FfArgs a) {
 
 // Few rows: a workgroup a row, in 32-bit floats, straight from the weights as they are.  What counts is the time from the first load to the last
 // store: no launch for fragments, and every wave has its loads on the way at once.  Columns lie along the lanes; the sum over the rows
-// of a matrix is shared by as many waves as there are left, and added up in LDS, always in the same order.  One row of 64 through 256: 7.5 us, of which a
-// launch and two round trips to memory are most (13.1 with fragments and eight waves).
+// of a matrix is shared by as many waves as there are left, and added up in LDS, always in the same order.  One row of 64 through 256: 8.0 us, of which a
+// launch and two round trips to memory are most (13.8 with fragments and eight waves).
 constexpr int kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kFewColumns = 1024, kFewMostF = 2048, kFewMostFo = 8192;
 template <int ACT>
 __global__ void __launch_bounds__(kFewThreads) k_ff_few(FfArgs a) {
@@ -613,11 +613,12 @@ struct Plan {
     part_floats = 2 * (int64_t)c.F * c.hidden + (int64_t)c.hidden * c.Fo + 2 * (int64_t)c.hidden + c.Fo;
     // Parts of the rows for the weights' gradients.  Rows of any width: a thousand workgroups, a tile of rows a wave at least.  Up to
     // 256 columns, where the tiles are of one snapshot each: as many workgroups (64 hidden columns each) as run at a time, and one tile each
-    // of up to 64, two of more, where there are few (64 columns through 256, backward: 37.7 us instead of 45.4 with four at 256 rows, 46.4
-    // instead of 47.8 at 4096, with one 48.9).
+    // of up to 64, two of more, where there are few (64 columns through 256, these gradients alone: 19.7 us instead of 28.0 with four at 256 rows, 27.6
+    // instead of 30.6 at 4096, with one 28.7).
     kept = c.F <= kKept && c.Fo <= kKept;
     const int64_t row_tiles = kept ? tiles(n, kTile) * k : tiles(rows, kTile);
-    // Eight waves share the rows' splitting where they are all of use (64 columns at most, for the registers): 0.87 of the time of four twice.
+    // Eight waves share the rows' splitting where they are all of use (64 columns at most, for the registers): 0.84 of the time of
+    // four twice at 32 columns, 0.92 at 64 (1.6 million rows, 128 and 256 hidden columns: 471 us, four 560; 1336, four 1451).
     const int64_t four = tiles(c.hidden, 64), eight = tiles(c.hidden, 128);
     weight_waves = std::max(ft, ot) <= 2 && 2 * eight * 87 < four * 100 ? 8 : 4;
     const int64_t at_a_time = weight_waves == 8 ? 256 : std::max(ft, ot) <= 2 ? 512 : std::max(ft, ot) <= 4 ? 256 : 128;
@@ -625,15 +626,15 @@ struct Plan {
     tiles_per_part = std::max<int64_t>(!kept ? 4 : row_tiles <= 64 ? 1 : 2, tiles(row_tiles, most));
     parts = tiles(row_tiles, tiles_per_part);
     // A workgroup a row takes as long for 256 rows, one a compute unit, as for one, and then for every further 256: 64 columns through 256,
-    // 7.5 us at 1 row, 8.2 at 256, 15.1 at 512; eight waves to 32 rows 13.1 to 14.1 throughout (32 through 128: 5.9, 6.5, 11.5 and 8.8 to
-    // 9.6; 256 through 1024: 48, 53, 97 and 76 to 81).  The kernels for more than 256 columns take longer for the same rows: 512 rows there (512
-    // through 2048: 185, 187, 369 at 512, 736 at 1024, in tiles 670 to 700; 40 through 512 to 600: 33, 35, 66, 130, in tiles 77 to 81).
+    // 8.1 us at 1 row, 8.5 at 256, 15.1 at 512; eight waves to 32 rows 13.8 to 14.1 throughout (32 through 128: 6.7, 7.0, 11.7 and 9.8 to
+    // 10.1; 256 through 1024: 47, 48, 95 and 89 to 92).  The kernels for more than 256 columns take longer for the same rows: 512 rows there (512
+    // through 2048: 185, 183, 363 at 512, 725 at 1024, in tiles 530 to 556; 40 through 600 to 512: 28, 29, 55, 109, in tiles 83 to 86).
     few = !backward && rows <= (kept ? 256 : 512) && c.F <= kFewMostF && (c.hidden <= kFewColumns || c.Fo <= kFewMostFo);  // (LDS holds a row, its sums)
     // Eight waves to 32 rows instead of one, as long as that is one round of workgroups: two a compute unit forward, one for the gradient of X,
-    // of which 256 columns need two for the same rows.  64 through 256, both with the packing of the weights: 13.8 us instead of 18.7 at
-    // 4096 rows, 16.1 instead of 19.7 at 16384, 24.7 instead of 20.7 at 32768; the gradient 19.5 instead of 27.7, 28.7 instead of 28.2 and
-    // 45.3 instead of 30.2.  256 through 1024 at 4096 rows: 78 instead of 160, the gradient 127 instead of 240.  Fewer than four tiles of
-    // hidden columns are too little to share: 16 through 64 took 8.5 instead of 8.1.
+    // of which 256 columns need two for the same rows.  64 through 256, both with the packing of the weights: 13.7 us instead of 20.5 at
+    // 4096 rows, 16.6 instead of 21.0 at 16384, 26.0 instead of 21.9 at 32768; the gradient 20.0 instead of 30.5 at 4096, 29.1 instead of 30.9 and
+    // 46.5 instead of 32.3.  256 through 1024 at 4096 rows: 84 instead of 186, the gradient 111 instead of 231.  Fewer than four tiles of
+    // hidden columns are too little to share: 16 through 64 took 8.8 instead of 8.2.
     const int64_t groups = backward ? tiles(rows, kTile) * tiles(ft, kKeptTiles) : tiles(rows, 2 * kTile);
     split = kept && ht >= 4 && groups <= kUnits;
     partial = take(backward ? (size_t)parts * part_floats * sizeof(float) : 0);

@@ -1,8 +1,8 @@
 // The gated feed-forward block, the gradient of X, on rows of up to 256 columns.
 //
-// 1.6 million rows of 64 through 256: 0.85 ms (308 TFLOP/s of its five products), the matrix instructions half and the vector ones 60 % of
-// the cycles.  More than 64 columns leave one wave a SIMD, which waits for its own instructions: 312 thousand rows of 128 through 341, 0.59 ms, 33 %
-// and 39 %.
+// 1.6 million rows of 64 through 256: 0.95 ms (277 TFLOP/s of its five products), the matrix instructions 44 % and the vector ones 66 % of
+// the cycles.  More than 64 columns leave one wave a SIMD, which waits for its own instructions: 312 thousand rows of 128 through 341, 0.67 ms, 28 %
+// and 38 %.
 #include "pipad_gated_ff.h"
 
 namespace pipad {

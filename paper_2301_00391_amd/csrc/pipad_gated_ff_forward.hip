@@ -1,8 +1,8 @@
 // The gated feed-forward block, forward, on rows of up to 256 columns.
 //
-// Bound by issue and power: activations, scales and pieces of H are four fifths of the cycles in vector instructions (1.6 million rows of 64
-// through 256 with gelu), the matrix instructions 44 % beside them, at 1.6 to 2 GHz.  That takes 604 us, 260 TFLOP/s of the block's own
-// products; 8 million rows of 64 through 171 with silu 2.08 ms, 253 TFLOP/s and 2.0 TB/s.
+// Bound by issue and power: activations, scales and pieces of H are 87 % of the cycles in vector instructions (1.6 million rows of 64 through 256 with
+// gelu), the matrix instructions 40 % beside them, at 1.8 GHz.  That takes 650 us, 242 TFLOP/s of the block's own products; 8 million rows of 64
+// through 171 with silu, 77 % and 45 % at 1.6 GHz, 2.21 ms, 238 TFLOP/s and 1.9 TB/s.
 #include "pipad_gated_ff.h"
 
 namespace pipad {

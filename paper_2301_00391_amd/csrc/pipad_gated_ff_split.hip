@@ -2,7 +2,7 @@
 // hidden tiles alone, and what it takes is the latency of its chain of loads and products, however few rows there are.  Here eight waves have
 // the same 32 rows and every eighth hidden tile each, and their results are added up in LDS, always in the same order.  The rows' pieces lie
 // in LDS, where every wave needs them; a tile's weights are read by one wave only and come straight from the caches.  At 4096 rows of 64
-// columns through 256 that is 13.8 us instead of 18.7 (the gradient 19.5 instead of 27.7), of which packing the weights takes 5.
+// columns through 256 that is 13.7 us instead of 20.5 (the gradient 20.0 instead of 30.5), of which packing the weights takes 5 to 7.
 #include "pipad_gated_ff.h"
 
 namespace pipad {

@@ -10,9 +10,8 @@
 // Of more than 128 columns a workgroup accumulates the gradients that go with 128 of X's and 128 of Y's, and another makes G, U and dH once more
 // for the rest: all of them do not fit the registers.
 //
-// 1.6 million rows of 64 through 256: 1.25 ms (252 TFLOP/s of its six products), a quarter of it the rows' pieces on their way through LDS, the vector
-// instructions 69 % of the cycles, the matrix instructions 36 %.  312 thousand rows of 128 through 341, where one wave a SIMD waits for itself: 1.25 ms,
-// 39 % and 19 %.
+// 1.6 million rows of 64 through 256: 1.33 ms (236 TFLOP/s of its six products), the vector instructions 71 % of the cycles, the matrix instructions
+// 30 %.  312 thousand rows of 128 through 341, where one wave a SIMD waits for itself: 1.25 ms, 50 % and 19 %.
 //
 // Everything is in 16 x 16 x 32 instructions: 16 columns a wave rather than 32 halve the registers for weights and gradients, so that two
 // waves share a SIMD and one's elementwise work runs beside the other's matrix instructions.
@@ -44,8 +43,9 @@ __device__ inline void add_product16(Sums16 &c, const Split &a, const Split &b) 
 __device__ inline float sum_of(const Sums16 &c, int r) { return fmaf(c.cross[r], 1.f / kWide, c.main[r]); }
 
 // The pieces of 32 rows of 32 D columns, two planes, and 1 over the rows' scales.  The 16-byte chunks of a row are permuted by its number, so that
-// 16 lanes that read a chunk of a row each, and 32 that read 8 bytes of eight rows, meet all 64 banks once: rows of 64 D bytes are 4 / D to the
-// 256 of all banks, and the chunks of those that lie on the same banks have to differ, for the loads that transpose in pairs.
+// 16 neighbouring lanes that read a chunk of a row each, and 32 that read 8 bytes of eight rows, meet all 64 banks once: rows of 64 D bytes are 4 / D
+// to the 256 of all banks, and the chunks of those that lie on the same banks have to differ, for the loads that transpose in pairs.  26 to 28 % of
+// the LDS cycles are counted as conflicts all the same, so that some access is not taken 16, or 32, neighbouring lanes at a time.
 template <int D>
 struct Slot {
   char plane[2][kTile * 64 * D];

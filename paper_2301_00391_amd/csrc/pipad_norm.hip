@@ -6,7 +6,7 @@
 // Everything about a node row is local to the row but the gradients of the vectors that all rows share, so one pass over the
 // matrices does it: a row lies in the registers of LPR lanes, its sums go over these lanes, and nothing is kept from the
 // forward pass but R' itself.  What is read and written once is all that there is to move: 5 matrices forward, 8 backward.
-// Memory bounds it: 8 million rows of 64, forward, 1.62 ms, 6.3 TB/s (a sum of two large arrays reaches 6.1); 4 million of 128, backward, 3.10 ms,
+// Memory bounds it: 8 million rows of 64, forward, 1.61 ms, 6.4 TB/s (a sum of two large arrays reaches 6.1); 4 million of 128, backward, 3.11 ms,
 // 5.3 TB/s from five matrices to three; 150 thousand of 253, column by column, 5.2 TB/s.
 #include "pipad_internal.h"
 
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(kBlock) k_residual_norm_backward(NormArgs a) {
   w_pre.load_or(a.w_pre, lane, F, 1.f);
 #pragma unroll
   for (int q = 0; q < kSums; ++q) acc[q].fill(0.f), rest[q].fill(0.f);
-  // A plain chain of additions would be off by more the more rows a lane has (4 million rows of 128: 3.5e-7 of the sums' size, so 1.0e-7).  A sum of few
+  // A plain chain of additions would be off by more the more rows a lane has (4 million rows of 128: 3.5e-7 of the sums' size, so 1.4e-7).  A sum of few
   // columns a lane carries what its additions round off, in `rest`, at no cost; of more columns, whose registers are short, 64 rows are added up by
   // themselves and then to `rest` (256 MB a matrix, as plain chains, so, and carried: 512 columns 398, 420 and 422 us, 1022 columns 612, 621 and 663,
   // 4096 columns 632, 595 and 636, 4094 columns 687, 760 and 813).
