@@ -57,7 +57,10 @@ class _Rows:
         self.raw, self.side = _current_raw_stream(self.index), None
         if stream is not None and int(stream.cuda_stream) != self.raw:
             self.raw = int(stream.cuda_stream)
-            self.side = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.raw, self.device)
+            if isinstance(stream, torch.cuda.Stream):
+                self.side = stream
+            else:  # (the default stream has no pointer to be known by)
+                self.side = torch.cuda.ExternalStream(self.raw, self.device) if self.raw else torch.cuda.default_stream(self.device)
 
     def empty(self, shape, dtype: torch.dtype = torch.float32, returned: bool = True) -> torch.Tensor:
         """Memory for a call on its stream.  The current stream's would not do for another one: the allocator gives again what has just been

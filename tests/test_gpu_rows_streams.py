@@ -70,7 +70,7 @@ def test_results_dropped_early_wait_for_the_current_stream(pipad):  # noqa: F811
     side.wait_stream(torch.cuda.current_stream())
     got = calls(pipad, W, b, X, dY, v, stream=side)
     torch.cuda.current_stream().wait_stream(side)
-    torch.cuda._sleep(20_000_000)  # (some ten milliseconds, in place of what reads the results)
+    torch.cuda._sleep(400_000_000)  # (a fifth of a second, in place of what reads the results)
     large = [t for t in got if t.numel() * 4 > 1 << 20]
     sizes, at = [t.numel() * 4 for t in large], {t.data_ptr() for t in large}
     assert len(large) == 7
@@ -81,3 +81,42 @@ def test_results_dropped_early_wait_for_the_current_stream(pipad):  # noqa: F811
     assert not busy or not any(t.data_ptr() in at for t in again)
     torch.cuda.synchronize()
     assert busy
+
+
+@pytest.mark.parametrize("wrapped", [False, True])
+def test_the_default_stream_from_another_one(pipad, wrapped):  # noqa: F811
+    W, b, X, dY, v = operands(True)
+    want = calls(pipad, W, b, X, dY, v)
+    torch.cuda.synchronize()
+
+    class Other:
+        cuda_stream = 0
+
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = calls(pipad, W, b, X, dY, v, stream=Other() if wrapped else torch.cuda.default_stream())
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
+def test_another_stream_within_a_graph(pipad):  # noqa: F811
+    """Calls that a captured stream hands to a second one, which is captured with it, and their memory: replayed beside eager work."""
+    W, b, X, dY, v = operands(False)
+    calls(pipad, W, b, X, dY, v)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        first = calls(pipad, W, b, X, dY, v, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        for t in calls(pipad, W, b, X, dY, v, stream=side)[::2]:  # (and some that are dropped at once)
+            del t
+        torch.cuda.current_stream().wait_stream(side)
+        second = calls(pipad, W, b, X, dY, v)
+    for replay in range(3):
+        X.normal_(generator=torch.Generator(device="cuda").manual_seed(replay))
+        want = calls(pipad, W, b, X, dY, v)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got in (first, second):
+            assert all(torch.equal(x, y) for x, y in zip(want, got)), replay
