@@ -16,6 +16,7 @@ import re
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -24,6 +25,8 @@ LIB = os.path.join(HERE, "libpipad.so")
 SOURCES = ["pipad_api.hip", "pipad_build.hip", "pipad_aggregate.hip", "pipad_transpose.hip",
            "pipad_norm.hip", "pipad_gated_ff.hip", "pipad_gated_ff_forward.hip", "pipad_gated_ff_backward.hip",
            "pipad_gated_ff_weights.hip", "pipad_gated_ff_split.hip", "pipad_ceilings.hip"]
+#: sources of many kernels that are compiled once for each activation (PIPAD_FF_ACT)
+PER_ACTIVATION = ("pipad_gated_ff_forward.hip", "pipad_gated_ff_backward.hip", "pipad_gated_ff_weights.hip")
 
 
 def hipcc() -> str:
@@ -60,16 +63,20 @@ def build(verbose: bool = False, defines=(), output: str = LIB) -> str:
     ]
     objs = []
     procs = []
-    for src in SOURCES:
-        obj = os.path.join(CSRC, src.replace(".hip", f".{os.getpid()}.o"))
-        cmd = [hipcc(), *flags, "-Rpass-analysis=kernel-resource-usage", "-c",
+    for src, act in [(s, a) for s in SOURCES for a in (range(4) if s in PER_ACTIVATION else ("",))]:  # (all at the same time)
+        own = [f"-DPIPAD_FF_ACT={act}"] if act != "" else []
+        obj = os.path.join(CSRC, src.replace(".hip", f"{act}.{os.getpid()}.o"))
+        cmd = [hipcc(), *flags, *own, "-Rpass-analysis=kernel-resource-usage", "-c",
                os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
-        procs.append((cmd, subprocess.Popen(cmd, stderr=subprocess.PIPE, text=True)))
+        said = tempfile.TemporaryFile("w+")  # (a pipe holds so little that a compiler would wait for its turn to be read)
+        procs.append((cmd, subprocess.Popen(cmd, stderr=said), said))
         objs.append(obj)
-    for cmd, p in procs:
-        _, err = p.communicate()
+    for cmd, p, said in procs:
+        p.wait()
+        said.seek(0)
+        err = said.read()
         if p.returncode != 0:
             sys.stderr.write(err)
             raise RuntimeError("hipcc failed: " + " ".join(cmd))

@@ -337,11 +337,14 @@ struct Kept {
   void (*kernel)(FfArgs);
   int waves;
 };
-Kept kept_forward(int act, int fq, int ot);
-Kept kept_backward(int act, int fq, int oq);
+template <int ACT>
+Kept kept_forward(int fq, int ot);
+template <int ACT>
+Kept kept_backward(int fq, int oq);
 Kept split_forward(int act, int ot);  // 32 rows a workgroup
 Kept split_backward(int act, int ft);
-Kept kept_weights(int act, int fd, int od, int waves);  // tiles of 32 columns; 4 waves, or up to 2 tiles 8
+template <int ACT>
+Kept kept_weights(int fd, int od, int waves);  // tiles of 32 columns; 4 waves, or up to 2 tiles 8
 
 }  // namespace ff
 }  // namespace pipad

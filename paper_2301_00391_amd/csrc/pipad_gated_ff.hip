@@ -680,6 +680,10 @@ using FfKernel = void (*)(FfArgs);
 #define PIPAD_FF_KERNELS(name, ...) \
   constexpr FfKernel name##_of[4][3] = {{name<0, 1>, name<0, 2>, name<0, __VA_ARGS__>}, {name<1, 1>, name<1, 2>, name<1, __VA_ARGS__>}, \
                                         {name<2, 1>, name<2, 2>, name<2, __VA_ARGS__>}, {name<3, 1>, name<3, 2>, name<3, __VA_ARGS__>}};
+static_assert(PIPAD_ACT_SIGMOID == 0 && PIPAD_ACT_RELU == 1 && PIPAD_ACT_GELU == 2 && PIPAD_ACT_SILU == 3, "the order below");
+constexpr Kept (*kept_forward_of[4])(int, int) = {kept_forward<0>, kept_forward<1>, kept_forward<2>, kept_forward<3>};
+constexpr Kept (*kept_backward_of[4])(int, int) = {kept_backward<0>, kept_backward<1>, kept_backward<2>, kept_backward<3>};
+constexpr Kept (*kept_weights_of[4])(int, int, int) = {kept_weights<0>, kept_weights<1>, kept_weights<2>, kept_weights<3>};
 constexpr FfKernel k_ff_few_of[4] = {k_ff_few<0>, k_ff_few<1>, k_ff_few<2>, k_ff_few<3>};
 PIPAD_FF_KERNELS(k_ff_rows, 4)
 PIPAD_FF_KERNELS(k_ff_rows_backward, 4)
@@ -706,7 +710,7 @@ int gated_ff_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, const float
   const int rc = pack(c, p, false, ws, st);
   if (rc != PIPAD_OK) return rc;
   if (p.kept) {
-    const Kept f = p.split ? split_forward(c.activation, p.ot) : kept_forward(c.activation, p.fq, p.ot);
+    const Kept f = p.split ? split_forward(c.activation, p.ot) : kept_forward_of[c.activation](p.fq, p.ot);
     hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, p.split ? kTile : kTile * f.waves)), dim3(f.waves * kWave), 0, st, a);
     PIPAD_HIP(hipGetLastError());
     return PIPAD_OK;
@@ -728,7 +732,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
     if (rc != PIPAD_OK) return rc;
     const FfArgs a = arguments(c, p, n, k, X, ldx, dY, lddy, dX, lddx, ws);
     if (dX && p.kept) {
-      const Kept f = p.split ? split_backward(c.activation, p.ft) : kept_backward(c.activation, p.fq, p.oq);
+      const Kept f = p.split ? split_backward(c.activation, p.ft) : kept_backward_of[c.activation](p.fq, p.oq);
       hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(p.rows, p.split ? kTile : kTile * f.waves), (unsigned)tiles(p.ft, kKeptTiles)),
                          dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());
@@ -739,7 +743,7 @@ int gated_ff_backward_launch(const pipad_gated_ff_t &c, int32_t n, int32_t k, co
       PIPAD_HIP(hipGetLastError());
     }
     if (grads && p.kept) {
-      const Kept f = kept_weights(c.activation, p.ft, p.ot, p.weight_waves);
+      const Kept f = kept_weights_of[c.activation](p.ft, p.ot, p.weight_waves);
       hipLaunchKernelGGL(f.kernel, dim3((unsigned)tiles(c.hidden, 16 * f.waves), (unsigned)p.parts, (unsigned)tiles(std::max(p.ft, p.ot), kKeptTiles)),
                          dim3(f.waves * kWave), 0, st, a);
       PIPAD_HIP(hipGetLastError());

@@ -90,13 +90,10 @@ Kept kept_backward_of(int fq, int oq) {
 }
 }  // namespace
 
-Kept kept_backward(int act, int fq, int oq) {
-  switch (act) {
-    case PIPAD_ACT_SIGMOID: return kept_backward_of<PIPAD_ACT_SIGMOID>(fq, oq);
-    case PIPAD_ACT_RELU: return kept_backward_of<PIPAD_ACT_RELU>(fq, oq);
-    case PIPAD_ACT_GELU: return kept_backward_of<PIPAD_ACT_GELU>(fq, oq);
-    default: return kept_backward_of<PIPAD_ACT_SILU>(fq, oq);
-  }
+// (a source of its own for each activation: a quarter of the kernels each, compiled side by side)
+template <>
+Kept kept_backward<PIPAD_FF_ACT>(int fq, int oq) {
+  return kept_backward_of<PIPAD_FF_ACT>(fq, oq);
 }
 
 }  // namespace ff

@@ -81,13 +81,10 @@ Kept kept_of(int fq, int ot) {
 }
 }  // namespace
 
-Kept kept_forward(int act, int fq, int ot) {
-  switch (act) {
-    case PIPAD_ACT_SIGMOID: return kept_of<PIPAD_ACT_SIGMOID>(fq, ot);
-    case PIPAD_ACT_RELU: return kept_of<PIPAD_ACT_RELU>(fq, ot);
-    case PIPAD_ACT_GELU: return kept_of<PIPAD_ACT_GELU>(fq, ot);
-    default: return kept_of<PIPAD_ACT_SILU>(fq, ot);
-  }
+// (a source of its own for each activation: a quarter of the kernels each, compiled side by side)
+template <>
+Kept kept_forward<PIPAD_FF_ACT>(int fq, int ot) {
+  return kept_of<PIPAD_FF_ACT>(fq, ot);
 }
 
 }  // namespace ff

@@ -381,13 +381,10 @@ Kept kept_weights_of(int fd, int od, int waves) {
 }
 }  // namespace
 
-Kept kept_weights(int act, int fd, int od, int waves) {
-  switch (act) {
-    case PIPAD_ACT_SIGMOID: return kept_weights_of<PIPAD_ACT_SIGMOID>(fd, od, waves);
-    case PIPAD_ACT_RELU: return kept_weights_of<PIPAD_ACT_RELU>(fd, od, waves);
-    case PIPAD_ACT_GELU: return kept_weights_of<PIPAD_ACT_GELU>(fd, od, waves);
-    default: return kept_weights_of<PIPAD_ACT_SILU>(fd, od, waves);
-  }
+// (a source of its own for each activation: a quarter of the kernels each, compiled side by side)
+template <>
+Kept kept_weights<PIPAD_FF_ACT>(int fd, int od, int waves) {
+  return kept_weights_of<PIPAD_FF_ACT>(fd, od, waves);
 }
 
 }  // namespace ff
